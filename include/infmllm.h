@@ -340,6 +340,162 @@ int infmllm_stream_profile_select(infmllm_stream_t* s, unsigned kernels);
  */
 int infmllm_stream_profile_read(infmllm_stream_t* s, float* ms, int* launches);
 
+/*
+ * ---- Rotary positions and head norms -----------------------------------------------------------
+ *
+ * A rotary object is what a model applies to its projected queries and keys: positions by rotation (half-split or
+ * neighbouring pairs, the whole head or its first part, frequencies scaled for contexts longer than the trained one) and,
+ * with weights, the norm of every head ahead of it.  Independent of streams, whose INFMLLM_PARAM_ROPE_BASE turns cached keys
+ * by their place in the cache.  One object serves all layers.
+ *
+ *   y  = x * w / sqrt(mean(x^2) + eps) over the head (no weights: y = x)
+ *   a' = m (a cos(p f) - b sin(p f)),  b' = m (b cos(p f) + a sin(p f))   for pair i of dims / 2 with frequency f = f[i]
+ *   f[i] = base^(-2i/dims) * (g + (1 - g) / factor),  g = clamp((trained * base^(-2i/dims) / 2 pi - low) / (high - low), 0, 1),
+ *          g = 0 with trained = 0: every frequency divided by factor
+ *
+ * Angles, cosines and sines are computed in 64 bits (a table, at attach), the rest in 32, and a value is rounded once.
+ */
+typedef struct infmllm_rotary infmllm_rotary_t; /* opaque, library-owned host object */
+
+enum {
+    INFMLLM_ROTARY_BASE = 0,      /* base > 1 of the angles; 0: no rotation (norms alone).  Default 10000                   */
+    INFMLLM_ROTARY_DIMS = 1,      /* leading dimensions of a head that are turned, a multiple of 16 in 16..head_dim (default);
+                                     the others pass                                                                       */
+    INFMLLM_ROTARY_LAYOUT = 2,    /* pairs: 0 (default) (x[i], x[i + dims/2]); 1 (x[2i], x[2i + 1])                          */
+    INFMLLM_ROTARY_FACTOR = 3,    /* what frequencies are divided by, >= 1 (default 1)                                      */
+    INFMLLM_ROTARY_TRAINED = 4,   /* positions the model was trained on: > 0 scales by parts, frequencies that make more than
+                                     `high` turns within it are kept and those below `low` divided whole.  Default 0        */
+    INFMLLM_ROTARY_LOW = 5,       /* `low` and `high`, in turns, 0 <= low < high at attach; defaults 1 and 32               */
+    INFMLLM_ROTARY_HIGH = 6,
+    INFMLLM_ROTARY_MAGNITUDE = 7, /* m > 0, on cosine and sine (not on dimensions that pass).  Default 1                     */
+    INFMLLM_ROTARY_EPS = 8        /* eps >= 0 of the norm.  Default 1e-6                                                     */
+};
+
+/*
+ * Creates a rotary object for heads of head_dim (64 or 128) elements of dtype and positions 0 .. max_positions - 1
+ * (1..2^24).  Host-only.  Errors: EINVAL, ENOMEM.
+ */
+int infmllm_rotary_create(int head_dim, int dtype, int max_positions, infmllm_rotary_t** out);
+
+/* Sets a parameter, before attach (ESTATE afterwards).  EINVAL for an unknown parameter or a value out of range. */
+int infmllm_rotary_set_param(infmllm_rotary_t* r, int which, double value);
+
+/* Bytes of device workspace: the table, 8 bytes per position and pair (0 if r is null). */
+size_t infmllm_rotary_workspace_bytes(const infmllm_rotary_t* r);
+
+/*
+ * Hands the object its workspace (256-byte aligned, caller-owned) and the HIP stream its calls are enqueued on, and enqueues
+ * the kernel that fills the table there.  A paged append (below) of another HIP stream that uses the object has to be ordered
+ * behind that by the caller.  Errors: EINVAL (null or misaligned workspace, low >= high), ENOMEM, ESTATE, EHIP.
+ */
+int infmllm_rotary_attach(infmllm_rotary_t* r, void* dev_workspace, size_t bytes, void* hip_stream);
+
+/*
+ * q_out[i] = the heads of q[i] normed and turned to position positions[i], k_out likewise, i < tokens (0: nothing happens).
+ *   positions   device, int32 [tokens]; the rows of a token outside 0 .. max_positions - 1 become NaN where they are turned
+ *   q, q_out    device, token i's `heads` heads of head_dim at i * q_stride (q_out_stride) elements, dense within the token.
+ *               May be null together with heads = 0
+ *   k, k_out    the same with kv_heads
+ *   q_weight    device, [head_dim] in the object's dtype: the norm's weights; null: no norm of the queries
+ *   k_weight    the same for the keys
+ * Data pointers are aligned to 16 bytes and strides are multiples of 16 bytes, at least a token's heads.  An output may be its
+ * input (same pointer and stride) and must not overlap the inputs otherwise.
+ * Errors: EINVAL, ESTATE (not attached), EHIP.
+ */
+int infmllm_rotary_apply(infmllm_rotary_t* r, const int32_t* positions, int tokens, int heads, int kv_heads,
+                         const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         const void* q_weight, const void* k_weight,
+                         void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride);
+
+/* Releases the host object (not the workspace).  Null is a no-op. */
+void infmllm_rotary_destroy(infmllm_rotary_t* r);
+
+/*
+ * ---- Paged caches ------------------------------------------------------------------------------
+ *
+ * Beside the streams, which hold one sequence to a budget: the whole cache of many sequences, in pages.  A paged object is the
+ * geometry and the workspace of such a cache, and serves all layers of a model; a layer's pools are arguments of the calls:
+ *
+ *   K, V        device, [pages][kv_heads][page_size][head_dim], caller-owned, 16-byte aligned, not overlapping.  Rows that
+ *               no sequence holds may contain anything, values that are not finite among them.
+ *
+ * A batch is what a model step brings: the new tokens of `seqs` sequences, one after the other, some with whole chunks,
+ * others with one token or none.  Its arrays are device memory that is read when the kernels run (so a captured graph
+ * follows them); what they hold cannot be checked on the host, and whatever it is, nothing outside the pools, the arrays and
+ * the outputs is touched:
+ *   - a page number outside 0 .. pages - 1: its keys are hidden, and nothing is appended there;
+ *   - a length beyond pages_per_seq * page_size: the keys past it are hidden, and nothing is appended there;
+ *   - a sequence with fewer cached tokens than new ones: the first of its new tokens have no position; they are not
+ *     appended, and see no key;
+ *   - tokens from starts[seqs] on belong to no sequence: their rows of all outputs are left as they were.
+ * Pages may be shared by sequences for reading; what two tokens of a call append to one row is one of the two.
+ */
+typedef struct infmllm_paged infmllm_paged_t; /* opaque, library-owned host object */
+
+typedef struct infmllm_batch {
+    int seqs;               /* 1..65536                                                                          */
+    int tokens;             /* rows of q, k, v, out; 0: nothing happens                                          */
+    int max_new;            /* upper bounds of a sequence's new tokens and of its length, for the choice of the   */
+    int max_len;            /*   launches: results are right, if slow, where the arrays exceed them              */
+    const int32_t* starts;  /* device, [seqs + 1], ascending from 0: sequence s has the tokens starts[s] .. starts[s + 1] - 1 */
+    const int32_t* lens;    /* device, [seqs]: tokens in the cache, the new ones included                         */
+    const int32_t* table;   /* device, [seqs][pages_per_seq]: the pages of a sequence in order                     */
+    int pages_per_seq;
+} infmllm_batch_t;
+
+enum {
+    INFMLLM_PAGED_SCALE = 0,  /* softmax scale on q.k; default 1/sqrt(head_dim)                                   */
+    INFMLLM_PAGED_WINDOW = 1  /* a token sees the newest `window` keys, itself included; 0 (default): all          */
+};
+
+/*
+ * Creates a paged object: pools of `pages` pages (1..2^30) of page_size rows (a power of two in 16..1024); heads, kv_heads,
+ * head_dim and dtype as for infmllm_stream_create.  Host-only.  Errors: EINVAL, ENOMEM.
+ */
+int infmllm_paged_create(int pages, int page_size, int heads, int kv_heads, int head_dim, int dtype, infmllm_paged_t** out);
+
+/* Sets a parameter, before attach (ESTATE afterwards).  EINVAL for an unknown parameter or a value out of range. */
+int infmllm_paged_set_param(infmllm_paged_t* p, int which, double value);
+
+/* Bytes of device workspace: scratch of key ranges that are shared by workgroups (0 if p is null). */
+size_t infmllm_paged_workspace_bytes(const infmllm_paged_t* p);
+
+/*
+ * Hands the object its workspace (256-byte aligned, caller-owned) and the HIP stream its calls are enqueued on, and clears the
+ * workspace there.  Calls of one object use the one workspace: a caller who replays captured graphs of them on other HIP streams
+ * keeps them from running at the same time.  Errors: EINVAL, ENOMEM, ESTATE, EHIP.
+ */
+int infmllm_paged_attach(infmllm_paged_t* p, void* dev_workspace, size_t bytes, void* hip_stream);
+
+/*
+ * The new tokens' keys and values become rows of the pools; token r of the n new ones of sequence s has position
+ * p = lens[s] - n + r and goes to row p % page_size of page table[s][p / page_size].  With a rotary object keys are normed
+ * (k_weight not null) and turned to p on the way, and the queries with them where q is given.
+ *   rotary      attached, of the same head_dim and dtype; null: keys enter as given, and q and the weights must be null
+ *   k, v        device, strided rows as for infmllm_rotary_apply;  q, q_out, weights likewise (q null: keys alone)
+ * Errors: EINVAL (also pointers or strides that are not multiples of 16 bytes), ECAPACITY (max_len beyond the rotary object's
+ * positions; tokens the arrays put there all the same become NaN where they are turned), ESTATE (not attached), EHIP.
+ */
+int infmllm_paged_append(infmllm_paged_t* p, infmllm_rotary_t* rotary, const infmllm_batch_t* batch,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* k_weight,
+                         const void* q, int64_t q_stride, const void* q_weight, void* q_out, int64_t q_out_stride,
+                         void* K, void* V);
+
+/*
+ * Attention of the new tokens over the pages, their own keys included (they have been appended): for the token at position p
+ *   out = softmax_j(scale * q.K[j]) V[j] over the keys j <= p, with a window j > p - window;  0 where it sees none
+ *   q      device, strided rows as for infmllm_rotary_apply;  out  device, [tokens][heads][head_dim].  It may be q where q is
+ *          dense, and must not overlap q otherwise
+ *   lse    device, float [tokens][heads]: log(sum_j exp(scale * q.K[j])), -inf where no key is seen.  May be null
+ * A hidden key or value reaches no result, whatever it is.  bf16: products with fp32 sums, weights of chunks rounded to bf16.
+ * Errors: EINVAL (also pointers or strides that are not multiples of 16 bytes), ESTATE (not attached), EHIP.
+ */
+int infmllm_paged_attend(infmllm_paged_t* p, const infmllm_batch_t* batch, const void* q, int64_t q_stride,
+                         const void* K, const void* V, void* out, float* lse);
+
+/* Releases the host object (not the workspace).  Null is a no-op. */
+void infmllm_paged_destroy(infmllm_paged_t* p);
+
 /* Message for the calling thread's most recent failure ("" if none).  Never null. */
 const char* infmllm_last_error(void);
 

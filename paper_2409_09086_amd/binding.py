@@ -25,7 +25,14 @@ EXPORTS = [
     "infmllm_stream_profile", "infmllm_stream_profile_read", "infmllm_decode", "infmllm_decode_n", "infmllm_stream_max_len",
     "infmllm_step_attend", "infmllm_stream_pending", "infmllm_evict_batched", "infmllm_stream_profile_select",
     "infmllm_stream_attach_static", "infmllm_stream_kernel",
+    "infmllm_rotary_create", "infmllm_rotary_set_param", "infmllm_rotary_workspace_bytes", "infmllm_rotary_attach",
+    "infmllm_rotary_apply", "infmllm_rotary_destroy",
+    "infmllm_paged_create", "infmllm_paged_set_param", "infmllm_paged_workspace_bytes", "infmllm_paged_attach",
+    "infmllm_paged_append", "infmllm_paged_attend", "infmllm_paged_destroy",
 ]
+ROTARY_BASE, ROTARY_DIMS, ROTARY_LAYOUT, ROTARY_FACTOR, ROTARY_TRAINED, ROTARY_LOW, ROTARY_HIGH, ROTARY_MAGNITUDE, ROTARY_EPS = range(9)
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+PAGED_SCALE, PAGED_WINDOW = 0, 1
 STATIC_WORKSPACE_BYTES = 64 << 20
 KERNELS = ["append", "attn", "score", "select", "compact", "decode", "rope", "evict"]
 
@@ -71,6 +78,24 @@ def lib():
         L.infmllm_stream_profile_read.argtypes = [P, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(I)]
         L.infmllm_stream_kernel.argtypes = [P, I, I, I]
         L.infmllm_stream_kernel.restype = ctypes.c_char_p
+        L.infmllm_rotary_create.argtypes = [I, I, I, ctypes.POINTER(P)]
+        L.infmllm_rotary_set_param.argtypes = [P, I, D]
+        L.infmllm_rotary_workspace_bytes.argtypes = [P]
+        L.infmllm_rotary_workspace_bytes.restype = ctypes.c_size_t
+        L.infmllm_rotary_attach.argtypes = [P, P, ctypes.c_size_t, P]
+        S = ctypes.c_int64
+        L.infmllm_rotary_apply.argtypes = [P, P, I, I, I, P, S, P, S, P, P, P, S, P, S]
+        L.infmllm_rotary_destroy.argtypes = [P]
+        L.infmllm_rotary_destroy.restype = None
+        L.infmllm_paged_create.argtypes = [I, I, I, I, I, I, ctypes.POINTER(P)]
+        L.infmllm_paged_set_param.argtypes = [P, I, D]
+        L.infmllm_paged_workspace_bytes.argtypes = [P]
+        L.infmllm_paged_workspace_bytes.restype = ctypes.c_size_t
+        L.infmllm_paged_attach.argtypes = [P, P, ctypes.c_size_t, P]
+        L.infmllm_paged_append.argtypes = [P, P, P, P, S, P, S, P, P, S, P, P, S, P, P]
+        L.infmllm_paged_attend.argtypes = [P, P, P, S, P, P, P, P]
+        L.infmllm_paged_destroy.argtypes = [P]
+        L.infmllm_paged_destroy.restype = None
         L.infmllm_last_error.restype = ctypes.c_char_p
         L.infmllm_stream_destroy.argtypes = [P]
         L.infmllm_stream_destroy.restype = None
@@ -300,3 +325,172 @@ def evict_batched(streams):
     # the gather is enqueued: torch's stream-ordered allocator may now recycle the chunk tensors
     for s in streams:
         s._held = None
+
+
+def _dtype_code(dtype):
+    code = {torch.bfloat16: BF16, torch.float32: FP32}.get(dtype)
+    if code is None:
+        raise ValueError("dtype must be torch.bfloat16 or torch.float32")
+    return code
+
+
+def _rows(t, dtype, tokens, heads, head_dim, name):
+    """Address and token stride of a [tokens, heads, head_dim] tensor whose tokens are dense."""
+    if t.dtype != dtype or not t.is_cuda:
+        raise ValueError("%s must be a device tensor of dtype %s" % (name, dtype))
+    if t.shape != (tokens, heads, head_dim):
+        raise ValueError("%s must have shape %s (got %s)" % (name, (tokens, heads, head_dim), tuple(t.shape)))
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (heads > 1 and s1 != head_dim):
+        raise ValueError("%s must be dense within a token" % name)
+    return t.data_ptr(), s0 if tokens > 1 else max(s0, heads * head_dim)
+
+
+def _weight(w, dtype, head_dim, name):
+    if w is None:
+        return None
+    if not w.is_cuda or w.dtype != dtype or w.shape != (head_dim,) or not w.is_contiguous():
+        raise ValueError("%s must be a contiguous device tensor of %d elements of dtype %s" % (name, head_dim, dtype))
+    return w.data_ptr()
+
+
+class _Attached:
+    """What objects with a workspace share: `prefix`_workspace_bytes, _attach and _destroy of a handle."""
+
+    def _attach(self, prefix, handle, device, hip_stream):
+        L = lib()
+        self._h, self._destroy = handle, getattr(L, prefix + "_destroy")
+        self.device = torch.device(device)
+        nbytes = getattr(L, prefix + "_workspace_bytes")(handle)
+        with torch.cuda.device(self.device):
+            self.hip_stream = hip_stream if hip_stream is not None else torch.cuda.current_stream(self.device).cuda_stream
+            self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+            aligned = (self.workspace.data_ptr() + 255) // 256 * 256
+            _check(getattr(L, prefix + "_attach")(handle, ctypes.c_void_p(aligned), nbytes, ctypes.c_void_p(self.hip_stream)))
+
+    def close(self):
+        h, self._h = getattr(self, "_h", None), None
+        if h and _lib is not None:
+            self._destroy(h)
+
+    def __del__(self):
+        self.close()
+
+
+class Rotary(_Attached):
+    """infmllm_rotary_t with its table: rotary positions and head norms.
+
+    base 0 or None: no rotation (norms alone); trained with factor, low_turns and high_turns: frequencies scaled by parts,
+    factor alone: all of them."""
+
+    def __init__(self, head_dim, max_positions, dtype=torch.bfloat16, base=10000.0, dims=None, layout="half", factor=None,
+                 trained=None, low_turns=None, high_turns=None, magnitude=None, norm_eps=None, device="cuda:0", hip_stream=None):
+        L = lib()
+        self.head_dim, self.max_positions, self.dtype = head_dim, max_positions, dtype
+        h = ctypes.c_void_p()
+        _check(L.infmllm_rotary_create(head_dim, _dtype_code(dtype), max_positions, ctypes.byref(h)))
+        self._h, self._destroy = h, L.infmllm_rotary_destroy
+        if layout not in ROTARY_LAYOUTS:
+            raise ValueError("layout must be one of %s" % sorted(ROTARY_LAYOUTS))
+        for which, val in ((ROTARY_BASE, base or 0.0), (ROTARY_DIMS, dims), (ROTARY_LAYOUT, ROTARY_LAYOUTS[layout]),
+                           (ROTARY_FACTOR, factor), (ROTARY_TRAINED, trained), (ROTARY_LOW, low_turns), (ROTARY_HIGH, high_turns),
+                           (ROTARY_MAGNITUDE, magnitude), (ROTARY_EPS, norm_eps)):
+            if val is not None:
+                _check(L.infmllm_rotary_set_param(h, which, float(val)))
+        self._attach("infmllm_rotary", h, device, hip_stream)
+
+    def apply(self, positions, q=None, k=None, q_weight=None, k_weight=None, q_out=None, k_out=None):
+        """infmllm_rotary_apply: q [n, heads, d], k [n, kv_heads, d] (either may be None), positions int32 [n].
+        Returns (q_out, k_out); q_out=q turns in place.  Nothing is synchronised."""
+        n, d, dt = positions.shape[0], self.head_dim, self.dtype
+        _dev_ptr(positions, torch.int32, (n,), "positions")
+        args = []
+        heads = []
+        outs = []
+        for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+            if x is None:
+                heads.append(0)
+                args.append((None, 0, None, 0))
+                outs.append(None)
+                continue
+            hx = x.shape[1]
+            if out is None:
+                out = torch.empty((n, hx, d), dtype=dt, device=x.device)
+            heads.append(hx)
+            args.append(_rows(x, dt, n, hx, d, name) + (_rows(out, dt, n, hx, d, name + "_out")))
+            outs.append(out)
+        (qp, qs, qo, qos), (kp, ks, ko, kos) = args
+        _check(lib().infmllm_rotary_apply(self._h, positions.data_ptr(), n, heads[0], heads[1], qp, qs, kp, ks,
+                                          _weight(q_weight, dt, d, "q_weight"), _weight(k_weight, dt, d, "k_weight"), qo, qos, ko, kos))
+        return outs[0], outs[1]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_int), ("tokens", ctypes.c_int), ("max_new", ctypes.c_int), ("max_len", ctypes.c_int),
+                ("starts", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("table", ctypes.c_void_p), ("pages_per_seq", ctypes.c_int)]
+
+
+class PagedBatch:
+    """infmllm_batch_t: the new tokens of a model step.  starts int32 [seqs + 1], lens int32 [seqs] (new tokens included), table
+    int32 [seqs, pages_per_seq] on the device; tokens, max_new and max_len (upper bounds) as the host knows them."""
+
+    def __init__(self, starts, lens, table, tokens, max_new, max_len):
+        seqs = lens.shape[0]
+        if table.dim() != 2:
+            raise ValueError("table must be two-dimensional")
+        _dev_ptr(starts, torch.int32, (seqs + 1,), "starts")
+        _dev_ptr(lens, torch.int32, (seqs,), "lens")
+        _dev_ptr(table, torch.int32, (seqs, table.shape[1]), "table")
+        self.starts, self.lens, self.table = starts, lens, table
+        self.tokens = int(tokens)
+        self._c = _Batch(seqs, self.tokens, int(max_new), int(max_len), starts.data_ptr(), lens.data_ptr(), table.data_ptr(), table.shape[1])
+        self._ref = ctypes.byref(self._c)
+
+
+class PagedCache(_Attached):
+    """infmllm_paged_t with its workspace: geometry and scratch of a paged cache; the pools of a layer, [pages, kv_heads,
+    page_size, head_dim] each, are the caller's and are arguments of every call (pools() makes a pair)."""
+
+    def __init__(self, pages, page_size, heads, kv_heads, head_dim, dtype=torch.bfloat16, scale=None, window=None, device="cuda:0",
+                 hip_stream=None):
+        L = lib()
+        self.heads, self.kv_heads, self.head_dim, self.dtype = heads, kv_heads, head_dim, dtype
+        self.pool_shape = (pages, kv_heads, page_size, head_dim)
+        h = ctypes.c_void_p()
+        _check(L.infmllm_paged_create(pages, page_size, heads, kv_heads, head_dim, _dtype_code(dtype), ctypes.byref(h)))
+        self._h, self._destroy = h, L.infmllm_paged_destroy
+        for which, val in ((PAGED_SCALE, scale), (PAGED_WINDOW, window)):
+            if val is not None:
+                _check(L.infmllm_paged_set_param(h, which, float(val)))
+        self._attach("infmllm_paged", h, device, hip_stream)
+
+    def pools(self):
+        """An uninitialised pair of pools (K, V)."""
+        return tuple(torch.empty(self.pool_shape, dtype=self.dtype, device=self.device) for _ in range(2))
+
+    def append(self, batch, k, v, K, V, rotary=None, k_weight=None, q=None, q_weight=None, q_out=None):
+        """infmllm_paged_append: k, v [tokens, kv_heads, d] enter the pools K, V; with a Rotary, keys and (where given) queries q
+        [tokens, heads, d] are normed and turned on the way.  Returns q_out (None without q).  Nothing is synchronised."""
+        n, d, dt = batch.tokens, self.head_dim, self.dtype
+        qp = qs = qo = qos = None
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty((n, self.heads, d), dtype=dt, device=q.device)
+            (qp, qs), (qo, qos) = _rows(q, dt, n, self.heads, d, "q"), _rows(q_out, dt, n, self.heads, d, "q_out")
+        (kp, ks), (vp, vs) = _rows(k, dt, n, self.kv_heads, d, "k"), _rows(v, dt, n, self.kv_heads, d, "v")
+        _check(lib().infmllm_paged_append(self._h, None if rotary is None else rotary._h, batch._ref, kp, ks, vp, vs,
+                                          _weight(k_weight, dt, d, "k_weight"), qp, qs or 0, _weight(q_weight, dt, d, "q_weight"), qo, qos or 0,
+                                          _dev_ptr(K, dt, self.pool_shape, "K"), _dev_ptr(V, dt, self.pool_shape, "V")))
+        return q_out if q is not None else None
+
+    def attend(self, batch, q, K, V, out=None, lse=None):
+        """infmllm_paged_attend: attention of q [tokens, heads, d] over the batch's pages.  Returns out [tokens, heads, d]; lse, float
+        [tokens, heads], receives the log-sum-exp.  Nothing is synchronised."""
+        n, d, dt = batch.tokens, self.head_dim, self.dtype
+        qp, qs = _rows(q, dt, n, self.heads, d, "q")
+        if out is None:
+            out = torch.empty((n, self.heads, d), dtype=dt, device=q.device)
+        _check(lib().infmllm_paged_attend(self._h, batch._ref, qp, qs, _dev_ptr(K, dt, self.pool_shape, "K"),
+                                          _dev_ptr(V, dt, self.pool_shape, "V"), _dev_ptr(out, dt, (n, self.heads, d), "out"),
+                                          _dev_ptr(lse, torch.float32, (n, self.heads), "lse")))
+        return out

@@ -13,15 +13,16 @@
 #include <string>
 #include <vector>
 
+#include "errors.h"
 #include "launch.h"
 
 using namespace infmllm;
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-int fail(int code, const char* fmt, ...)
+int infmllm::fail(int code, const char* fmt, ...)
 {
     char buf[512];
     va_list ap;
@@ -32,10 +33,12 @@ int fail(int code, const char* fmt, ...)
     return code;
 }
 
-int fail_hip(hipError_t e, const char* what)
+int infmllm::fail_hip(hipError_t e, const char* what)
 {
     return fail(INFMLLM_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+namespace {
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb)
 {

@@ -1,0 +1,45 @@
+// Internal launch interface of the rotary and paged-cache kernels.  Everything is asynchronous on the given HIP stream.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace infmllm {
+
+struct RotaryFrequencies { double base, factor, trained, low, high, magnitude; };
+
+// One launch over tokens x (query heads, key heads, value heads with pages); see rotary.hip.  T: uint16_t (bf16) or float.
+template <typename T>
+struct RotaryArgs {
+    const T *q, *k, *v;                            // strides in elements between tokens
+    T *q_out, *k_out;
+    const T *q_weight, *k_weight;                  // null: no norm
+    int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+    const int32_t* positions;                      // without pages
+    const float2* table_cs;                        // [max_positions][dims / 2] (cos, sin)
+    int tokens, heads, kv_heads, dims, half, max_positions;   // dims 0: nothing is turned; half: pairs (i, i + dims / 2)
+    float eps;
+    // with pages (see infmllm_batch_t)
+    const int32_t *starts, *lens, *table;
+    T *K, *V;
+    int seqs, pages_per_seq, pages, page_shift;
+};
+template <typename T>
+hipError_t launch_rotary(const RotaryArgs<T>& a, int head_dim, bool paged, hipStream_t st);
+hipError_t launch_rotary_table(float* tab, int half_dims, int positions, const RotaryFrequencies& f, hipStream_t st);
+
+// Attention over pages.
+template <typename T>
+struct PagedArgs {
+    const T* q;                                    // [tokens][..]: q_stride elements between tokens
+    const T *K, *V;                                // [pages][Hkv][1 << page_shift][D]
+    T* out;                                        // [tokens][Hq][D]
+    float* lse;                                    // [tokens][Hq] natural, or null
+    const int32_t *starts, *lens, *table;
+    int64_t q_stride;
+    int seqs, tokens, pages_per_seq, pages, page_shift, Hq, Hkv, G, window;   // window 0: none
+    float c;                                       // scale * log2(e)
+};
+template <typename T>
+hipError_t launch_paged_attend(const PagedArgs<T>& a, int head_dim, int max_new, int max_len, hipStream_t st);
+
+}  // namespace infmllm

@@ -488,7 +488,8 @@ int infmllm_paged_append(infmllm_paged_t* p, infmllm_rotary_t* rotary, const inf
  *          dense, and must not overlap q otherwise
  *   lse    device, float [tokens][heads]: log(sum_j exp(scale * q.K[j])), -inf where no key is seen.  May be null
  * A hidden key or value reaches no result, whatever it is.  bf16: products with fp32 sums, weights of chunks rounded to bf16.
- * Errors: EINVAL (also pointers or strides that are not multiples of 16 bytes), ESTATE (not attached), EHIP.
+ * Errors: EINVAL (also pointers or strides that are not multiples of 16 bytes, tokens * heads / kv_heads above 2^30), ESTATE (not
+ * attached), EHIP.
  */
 int infmllm_paged_attend(infmllm_paged_t* p, const infmllm_batch_t* batch, const void* q, int64_t q_stride,
                          const void* K, const void* V, void* out, float* lse);

@@ -39,7 +39,14 @@ struct PagedArgs {
     int seqs, tokens, pages_per_seq, pages, page_shift, Hq, Hkv, G, window;   // window 0: none
     float c;                                       // scale * log2(e)
 };
+// Partial results of units that several teams share (paged_work.h): two slots a team, and a ticket for each, zero between launches.
+struct PagedScratch { float* part; int* arrived; };
+constexpr int PAGED_CUS = 256;                     // compute units: teams of a launch with one a CU
+constexpr int PAGED_TEAMS = 8 * PAGED_CUS;         // most teams of a launch
+
+// The sequences with row_lo < new tokens * G <= row_hi; max_new: the caller's bound.
 template <typename T>
-hipError_t launch_paged_attend(const PagedArgs<T>& a, int head_dim, int max_new, int max_len, hipStream_t st);
+hipError_t launch_paged_rows(const PagedArgs<T>& a, const PagedScratch& sc, int head_dim, int max_new, int row_lo, int row_hi, hipStream_t st);
+size_t paged_rows_scratch(int head_dim, int elt);  // bytes of PagedScratch::part
 
 }  // namespace infmllm

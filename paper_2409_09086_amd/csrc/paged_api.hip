@@ -2,6 +2,7 @@
 // launches.  No device memory is allocated here and nothing synchronises.
 #include "../../include/infmllm.h"
 
+#include <climits>
 #include <cmath>
 #include <new>
 
@@ -96,7 +97,9 @@ struct infmllm_paged {
     hipStream_t st = nullptr;
 
     int elt() const { return dtype == INFMLLM_BF16 ? 2 : 4; }
-    size_t bytes() const { return ALIGN; }
+    PagedScratch sc{nullptr, nullptr};
+    size_t part_bytes() const { return up(paged_rows_scratch(d, elt())); }
+    size_t bytes() const { return up(PAGED_TEAMS * sizeof(int)) + part_bytes(); }
 };
 
 extern "C" {
@@ -281,7 +284,9 @@ int infmllm_paged_attach(infmllm_paged_t* p, void* ws, size_t bytes, void* hip_s
     if (bytes < p->bytes()) return fail(INFMLLM_ENOMEM, "paged_attach: workspace has %zu bytes, %zu needed", bytes, p->bytes());
     hipError_t e = hipGetDevice(&p->dev);
     if (e != hipSuccess) return fail_hip(e, "paged_attach: hipGetDevice");
-    if ((e = launch_zero(ws, p->bytes(), (hipStream_t)hip_stream)) != hipSuccess) return fail_hip(e, "paged_attach: clearing the workspace");
+    const size_t tickets = p->bytes() - p->part_bytes();
+    if ((e = launch_zero(ws, tickets, (hipStream_t)hip_stream)) != hipSuccess) return fail_hip(e, "paged_attach: clearing the workspace");
+    p->sc = PagedScratch{(float*)((char*)ws + tickets), (int*)ws};
     p->st = (hipStream_t)hip_stream;
     p->attached = true;
     return INFMLLM_OK;
@@ -345,6 +350,8 @@ int infmllm_paged_attend(infmllm_paged_t* p, const infmllm_batch_t* batch, const
     if ((rc = check_rows(who, "q", q, q_stride, p->Hq, p->d, elt)) || (rc = check_rows(who, "out", out, (int64_t)p->Hq * p->d, p->Hq, p->d, elt)))
         return rc;
     if (!K || !V || ((uintptr_t)K | (uintptr_t)V) % 16) return fail(INFMLLM_EINVAL, "%s: K and V must not be null and be aligned to 16 bytes", who);
+    if ((int64_t)batch->tokens * (p->Hq / p->Hkv) > (1 << 30))
+        return fail(INFMLLM_EINVAL, "%s: tokens * heads / kv_heads must not exceed 2^30", who);
     if ((uintptr_t)lse % 4) return fail(INFMLLM_EINVAL, "%s: lse must be aligned to 4 bytes", who);
     OnDevice on(p->dev);
     if (on.err != hipSuccess) return fail_hip(on.err, who);
@@ -357,7 +364,7 @@ int infmllm_paged_attend(infmllm_paged_t* p, const infmllm_batch_t* batch, const
         a.seqs = batch->seqs; a.tokens = batch->tokens; a.pages_per_seq = batch->pages_per_seq; a.pages = p->pages; a.page_shift = p->page_shift;
         a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv; a.window = p->window;
         a.c = (float)(p->scale * 1.4426950408889634);
-        return launch_paged_attend<T>(a, p->d, batch->max_new, batch->max_len, p->st);
+        return launch_paged_rows<T>(a, p->sc, p->d, batch->max_new, 0, INT_MAX, p->st);
     };
     const hipError_t e = elt == 2 ? go((uint16_t*)nullptr) : go((float*)nullptr);
     return e == hipSuccess ? INFMLLM_OK : fail_hip(e, who);

@@ -1,0 +1,173 @@
+// How the attention over pages is shared out (device side).
+//
+// A unit is (sequence, kv-head, R consecutive query rows); the rows of a kv-head are numbered token * G + head in group, so
+// that a group's heads share every key.  Nothing about the sequences is known on the host.  Every team (a workgroup or a
+// wavefront) therefore reads the batch's arrays itself, adds up what all units cost and takes its share of the whole, from
+// where the shares of the teams before it end: the chip is filled evenly whatever the lengths are, a long sequence is cut over
+// many teams, and a team has at most two units that others work on too, its first and its last.  Those leave
+// their partial results (un-normalised output, reference, sum) in the team's two slots, and the team that arrives last merges
+// the unit's pieces in their order, so that results do not depend on who that is.
+//
+// A unit costs its keys and OVERHEAD keys for queries and output, in whole numbers far below 2^53, held in doubles (64-bit
+// divisions in integers take a microsecond).  Shares are cut anywhere; the cut is rounded down to a run of keys, alike on both
+// sides of it.
+#pragma once
+#include "paged.h"
+
+namespace infmllm {
+namespace {
+
+constexpr int WORK_OVERHEAD = 64;
+
+struct Unit {
+    int first;         // token of row 0 of the sequence
+    int G, rows;       // rows of the sequence's kv-head
+    int pos0;          // position of that token (negative: it and some more have none)
+    int seq, h, row0;  // this unit: rows row0 .. row0 + R - 1
+    int kb, ke;        // keys that any of its rows sees
+    int r0, r1;        // the team's runs of RUN keys of it, counted from align(kb)
+    int pieces, piece, team0;   // the teams that share it: team0 + 0 .. pieces - 1; this is number `piece`
+    __device__ __forceinline__ int pos(int row) const { return pos0 + row / G; }
+};
+
+// R rows a unit; keys in runs of RUN from a multiple of RUN.
+template <int R, int RUN>
+struct Work {
+    const int32_t *starts, *lens;
+    int seqs, tokens, G, Hkv, window, row_lo, row_hi, team, teams;
+    int most_keys;             // what a sequence's row of the page table holds
+    double chunk, left, off, u0;   // of a share; left of mine; where in the unit I am; where the unit starts
+    int seq, h, tile;
+    int first, n, pos0, ntile;     // of the sequence
+    double base, inc;              // tile i of it costs base + (i + 1) * inc
+
+    struct Seq { int first, n, pos0, ntile; double base, inc; };
+    __device__ __forceinline__ Seq load(int s) const
+    {
+        const int s0 = starts[s], s1 = starts[s + 1], len = max(lens[s], 0);
+        return describe(s0, s1, len);
+    }
+    __device__ __forceinline__ Seq describe(int s0, int s1, int len) const
+    {
+        Seq q;
+        q.first = min(max(s0, 0), tokens);
+        q.n = max(min(s1, tokens) - q.first, 0);
+        const int64_t rows = (int64_t)q.n * G;
+        if (rows <= row_lo || rows > row_hi) q.n = 0;
+        q.pos0 = q.n > 0 ? len - (s1 - q.first) : 0;
+        q.ntile = (int)((q.n * (int64_t)G + R - 1) / R);
+        const int ctx = min(max(q.pos0, 0), most_keys), step = max(R / G, 1);
+        if (window > 0) { q.base = (double)WORK_OVERHEAD + min((double)ctx + q.n, (double)window + step); q.inc = 0.0; }
+        else { q.base = (double)WORK_OVERHEAD + ctx; q.inc = (double)step; }
+        return q;
+    }
+    static __device__ __forceinline__ double before(const Seq& q, int i) { return i * q.base + q.inc * (0.5 * i * (i + 1.0)); }
+    __device__ __forceinline__ double of_head(const Seq& q) const { return q.n > 0 ? before(q, q.ntile) : 0.0; }
+    __device__ __forceinline__ void take(const Seq& q) { first = q.first; n = q.n; pos0 = q.pos0; ntile = q.ntile; base = q.base; inc = q.inc; }
+
+    __device__ Work() = default;
+    // All lanes of the wavefront call this.  teams: how many share the work; least: the smallest share, in keys.
+    template <typename T>
+    __device__ __forceinline__ Work(const PagedArgs<T>& a, int team_, int teams_, int least, int row_lo_, int row_hi_, int lane)
+        : starts(a.starts), lens(a.lens), seqs(a.seqs), tokens(a.tokens), G(a.G), Hkv(a.Hkv), window(a.window), row_lo(row_lo_),
+          row_hi(row_hi_), team(team_), teams(teams_)
+    {
+        most_keys = (int)min((int64_t)a.pages_per_seq << a.page_shift, (int64_t)INT32_MAX - 65536);
+        const int per = (seqs + 63) / 64;                      // consecutive sequences of a lane
+        double mine = 0.0;
+        Seq q{};
+        for (int i = 0; i < per; ++i) {
+            const int s = lane * per + i;
+            if (s < seqs) { q = load(s); mine += of_head(q) * Hkv; }
+        }
+        double incl = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const double x = __shfl_up(incl, d);
+            if (lane >= d) incl += x;
+        }
+        const double total = uniform(__shfl(incl, 63));
+        chunk = fmax(ceil(total / teams), (double)least);
+        const double lo = team * chunk;
+        left = fmin(chunk, total - lo);
+        if (!(left > 0.0)) { left = 0.0; return; }
+        const int who = __builtin_ctzll(__ballot(incl > lo));
+        double rem = lo - uniform(__shfl(incl - mine, who));
+        seq = who * per;
+        Seq now;
+        for (;;) {                                             // the sequence in that lane's block
+            if (per == 1) {
+                now.first = __builtin_amdgcn_readlane(q.first, who); now.n = __builtin_amdgcn_readlane(q.n, who);
+                now.pos0 = __builtin_amdgcn_readlane(q.pos0, who); now.ntile = __builtin_amdgcn_readlane(q.ntile, who);
+                now.base = uniform(__shfl(q.base, who)); now.inc = uniform(__shfl(q.inc, who));
+                break;
+            }
+            now = load(seq);
+            const double c = of_head(now) * Hkv;
+            if (rem < c || seq + 1 >= seqs) break;
+            rem -= c;
+            ++seq;
+        }
+        take(now);
+        const double head = of_head(now);
+        h = (int)(rem / head);
+        rem -= h * head;
+        // the tile: the largest i whose predecessors cost no more than rem
+        const double bb = now.base + 0.5 * now.inc;
+        int i = now.inc > 0.0 ? (int)((sqrt(bb * bb + 2.0 * now.inc * rem) - bb) / now.inc) : (int)(rem / now.base);
+        i = min(max(i, 0), ntile - 1);
+        while (i > 0 && before(now, i) > rem) --i;
+        while (i + 1 < ntile && before(now, i + 1) <= rem) ++i;
+        tile = __builtin_amdgcn_readfirstlane(i);
+        h = __builtin_amdgcn_readfirstlane(h);
+        off = uniform(rem - before(now, tile));
+        u0 = lo - off;
+    }
+    static __device__ __forceinline__ double uniform(double x)
+    {
+        const uint64_t u = __builtin_bit_cast(uint64_t, x);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    }
+    // The next piece of my share; false: there is none.
+    __device__ __forceinline__ bool next(Unit& u)
+    {
+        if (!(left > 0.0)) return false;
+        const double cost = base + (tile + 1) * inc, take_ = fmin(cost - off, left), end = off + take_;
+        u.first = first; u.G = G; u.rows = n * G; u.pos0 = pos0; u.seq = seq; u.h = h; u.row0 = tile * R;
+        const int last = min(u.row0 + R, u.rows) - 1;
+        u.ke = min(max(u.pos(last) + 1, 0), most_keys);
+        u.kb = window > 0 ? min(max(u.pos(u.row0) + 1 - window, 0), u.ke) : 0;
+        const int runs = (u.ke - (u.kb & ~(RUN - 1)) + RUN - 1) / RUN;
+        u.r0 = 0; u.r1 = runs; u.pieces = 1; u.piece = 0; u.team0 = team;
+        if (off > 0.0 || end < cost) {
+            if (off > 0.0) u.r0 = (int)(runs * off / cost);
+            if (end < cost) u.r1 = (int)(runs * end / cost);
+            u.team0 = min(max((int)(u0 / chunk), 0), team);
+            u.pieces = min((int)((u0 + cost - 1.0) / chunk), teams - 1) - u.team0 + 1;
+            u.piece = team - u.team0;
+        }
+        auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
+        scalar(u.first); scalar(u.rows); scalar(u.pos0); scalar(u.seq); scalar(u.h); scalar(u.row0); scalar(u.kb); scalar(u.ke);
+        scalar(u.r0); scalar(u.r1); scalar(u.pieces); scalar(u.piece); scalar(u.team0);
+        left -= take_;
+        off = 0.0;
+        u0 += cost;
+        if (left > 0.0 && ++tile == ntile) {
+            tile = 0;
+            if (++h == Hkv) {
+                h = 0;
+                do {
+                    if (++seq >= seqs) { left = 0.0; break; }
+                    take(load(seq));
+                } while (n == 0);
+            }
+        }
+        return true;
+    }
+    // which of a team's two slots a piece of a shared unit uses: the unit it ends with, or the one it begins with
+    static __device__ __forceinline__ int slot(const Unit& u, int piece) { return 2 * (u.team0 + piece) + (piece == 0 ? 1 : 0); }
+};
+
+}  // namespace
+}  // namespace infmllm

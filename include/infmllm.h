@@ -450,7 +450,8 @@ enum {
 
 /*
  * Creates a paged object: pools of `pages` pages (1..2^30) of page_size rows (a power of two in 16..1024); heads, kv_heads,
- * head_dim and dtype as for infmllm_stream_create.  Host-only.  Errors: EINVAL, ENOMEM.
+ * head_dim and dtype as for infmllm_stream_create, at most 65536 heads and 4096 of a group, and pages of all kv-heads below 2^29
+ * elements.  Host-only.  Errors: EINVAL, ENOMEM.
  */
 int infmllm_paged_create(int pages, int page_size, int heads, int kv_heads, int head_dim, int dtype, infmllm_paged_t** out);
 

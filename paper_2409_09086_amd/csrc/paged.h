@@ -37,6 +37,7 @@ struct PagedArgs {
     const int32_t *starts, *lens, *table;
     int64_t q_stride;
     int seqs, tokens, pages_per_seq, pages, page_shift, Hq, Hkv, G, window;   // window 0: none
+    uint32_t inv_g;                                // 2^32 / G + 1, rounded down (G > 1): see Unit::token
     float c;                                       // scale * log2(e)
 };
 // Partial results of units that several teams share (paged_work.h): two slots a team, and a ticket for each, zero between launches.
@@ -48,5 +49,8 @@ constexpr int PAGED_TEAMS = 8 * PAGED_CUS;         // most teams of a launch
 template <typename T>
 hipError_t launch_paged_rows(const PagedArgs<T>& a, const PagedScratch& sc, int head_dim, int max_new, int row_lo, int row_hi, hipStream_t st);
 size_t paged_rows_scratch(int head_dim, int elt);  // bytes of PagedScratch::part
+// The same for bf16 chunks of many rows, 256 a unit.
+hipError_t launch_paged_fwd(const PagedArgs<uint16_t>& a, const PagedScratch& sc, int head_dim, int row_lo, int row_hi, hipStream_t st);
+size_t paged_fwd_scratch(int head_dim);
 
 }  // namespace infmllm

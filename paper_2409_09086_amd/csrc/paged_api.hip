@@ -2,6 +2,7 @@
 // launches.  No device memory is allocated here and nothing synchronises.
 #include "../../include/infmllm.h"
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <new>
@@ -98,7 +99,7 @@ struct infmllm_paged {
 
     int elt() const { return dtype == INFMLLM_BF16 ? 2 : 4; }
     PagedScratch sc{nullptr, nullptr};
-    size_t part_bytes() const { return up(paged_rows_scratch(d, elt())); }
+    size_t part_bytes() const { return up(std::max(paged_rows_scratch(d, elt()), dtype == INFMLLM_BF16 ? paged_fwd_scratch(d) : 0)); }
     size_t bytes() const { return up(PAGED_TEAMS * sizeof(int)) + part_bytes(); }
 };
 
@@ -241,9 +242,12 @@ int infmllm_paged_create(int pages, int page_size, int heads, int kv_heads, int 
         return fail(INFMLLM_EINVAL, "paged_create: page_size must be a power of two in 16..1024 (got %d)", page_size);
     if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || heads > 65536)
         return fail(INFMLLM_EINVAL, "paged_create: kv_heads must divide heads, at most 65536 (got %d, %d)", heads, kv_heads);
+    if (heads / kv_heads > 4096) return fail(INFMLLM_EINVAL, "paged_create: at most 4096 heads share a kv-head (got %d)", heads / kv_heads);
     if (head_dim != 64 && head_dim != 128)
         return fail(INFMLLM_EINVAL, "paged_create: head_dim must be 64 or 128 (got %d)", head_dim);
     if (dtype != INFMLLM_BF16 && dtype != INFMLLM_FP32) return fail(INFMLLM_EINVAL, "paged_create: unknown dtype %d", dtype);
+    if ((int64_t)kv_heads * page_size * head_dim * 4 > INT_MAX)
+        return fail(INFMLLM_EINVAL, "paged_create: a page of %d rows of %d heads is too large", page_size, kv_heads);
     infmllm_paged* p = new (std::nothrow) infmllm_paged();
     if (!p) return fail(INFMLLM_ENOMEM, "paged_create: out of host memory");
     p->pages = pages; p->page_size = page_size; p->page_shift = __builtin_ctz((unsigned)page_size);
@@ -363,7 +367,18 @@ int infmllm_paged_attend(infmllm_paged_t* p, const infmllm_batch_t* batch, const
         a.q_stride = q_stride;
         a.seqs = batch->seqs; a.tokens = batch->tokens; a.pages_per_seq = batch->pages_per_seq; a.pages = p->pages; a.page_shift = p->page_shift;
         a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv; a.window = p->window;
+        a.inv_g = (uint32_t)((1ull << 32) / (unsigned)a.G + 1);
         a.c = (float)(p->scale * 1.4426950408889634);
+        if constexpr (sizeof(T) == 2) {
+            // Chunks of more than a few rows run 256 rows a unit; sequences beside them whose rows are one block of 16 run on their own.
+            const int new_max = std::min(batch->max_new, batch->tokens), few = 16;
+            if ((int64_t)new_max * a.G > 2 * few) {
+                const bool alike = a.seqs == 1 || (int64_t)new_max * a.seqs == a.tokens;
+                hipError_t e = hipSuccess;
+                if (!alike) e = launch_paged_rows<T>(a, p->sc, p->d, 1, 0, few, p->st);
+                return e != hipSuccess ? e : launch_paged_fwd(a, p->sc, p->d, alike ? 0 : few, INT_MAX, p->st);
+            }
+        }
         return launch_paged_rows<T>(a, p->sc, p->d, batch->max_new, 0, INT_MAX, p->st);
     };
     const hipError_t e = elt == 2 ? go((uint16_t*)nullptr) : go((float*)nullptr);

@@ -86,25 +86,27 @@ __device__ __forceinline__ void plain_row(const PagedArgs<T>& a, int seq, int h,
     }
 }
 
-// The query row `row` (of the sequence's kv-head rows) of a unit.
+// The query of row r of a unit.
 template <typename T, int D>
-__device__ __forceinline__ const T* query_of(const PagedArgs<T>& a, const Unit& u, int row)
+__device__ __forceinline__ const T* query_of(const PagedArgs<T>& a, const Unit& u, int r)
 {
-    const int tok = row / u.G;
-    return a.q + (int64_t)(u.first + tok) * a.q_stride + (int64_t)(u.h * u.G + row - tok * u.G) * D;
+    int head;
+    const int tok = u.token(r, head);
+    return a.q + (int64_t)(u.first + tok) * a.q_stride + (int64_t)(u.h * u.G + head) * D;
 }
 // The same row of out and lse: its number among [tokens][Hq].
 template <typename T>
-__device__ __forceinline__ int64_t result_of(const PagedArgs<T>& a, const Unit& u, int row)
+__device__ __forceinline__ int64_t result_of(const PagedArgs<T>& a, const Unit& u, int r)
 {
-    const int tok = row / u.G;
-    return (int64_t)(u.first + tok) * a.Hq + u.h * u.G + row - tok * u.G;
+    int head;
+    const int tok = u.token(r, head);
+    return (int64_t)(u.first + tok) * a.Hq + u.h * u.G + head;
 }
-// Keys of runs r0 .. r1 - 1 of a unit that a row sees: k0 .. k1 - 1.
+// Keys of runs r0 .. r1 - 1 of a unit that its row r sees: k0 .. k1 - 1.
 template <int RUN>
-__device__ __forceinline__ void visible(const Unit& u, int window, int row, int& k0, int& k1)
+__device__ __forceinline__ void visible(const Unit& u, int window, int r, int& k0, int& k1)
 {
-    const int pos = u.pos(row), at = u.kb & ~(RUN - 1);
+    const int pos = u.pos(r), at = u.kb & ~(RUN - 1);
     k0 = max(max(window > 0 ? pos + 1 - window : 0, at + u.r0 * RUN), u.kb);
     k1 = min(min(pos + 1, at + u.r1 * RUN), u.ke);
 }

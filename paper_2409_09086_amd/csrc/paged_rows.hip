@@ -97,7 +97,7 @@ struct RowsKernel<uint16_t, D, NRB> {
         int hi[NRB], lo[NRB];
 #pragma unroll
         for (int x = 0; x < NRB; ++x) {
-            const int row = min(u.row0 + 16 * x + c16, u.rows - 1);
+            const int row = min(16 * x + c16, u.rows - u.row0 - 1);
             const T* qp = query_of<T, D>(a, u, row) + 8 * g4;
             hi[x] = u.pos(row);
             lo[x] = a.window > 0 ? hi[x] + 1 - a.window : 0;
@@ -253,7 +253,7 @@ struct RowsKernel<float, D, 1> {
             if (np > 1) runs.look_up(k_first + step);
         }
         f32x4 qf[NJ];
-        const int row = min(u.row0 + c16, u.rows - 1), hi = u.pos(row), lo = a.window > 0 ? hi + 1 - a.window : 0;
+        const int row = min(c16, u.rows - u.row0 - 1), hi = u.pos(row), lo = a.window > 0 ? hi + 1 - a.window : 0;
         {
             const float* qp = query_of<T, D>(a, u, row) + 4 * g4;
 #pragma unroll
@@ -410,9 +410,9 @@ paged_rows_kernel(PagedArgs<T> a, PagedScratch sc, int least, int row_lo, int ro
             sync();
             for (int r = wave; r < rows; r += TW) {
                 int k0, k1;
-                visible<KEYS>(u, a.window, u.row0 + r, k0, k1);
+                visible<KEYS>(u, a.window, r, k0, k1);
                 float m, l, o[D / 64];
-                plain_row<T, D>(a, u.seq, u.h, query_of<T, D>(a, u, u.row0 + r), k0, k1, lane, m, l, o);
+                plain_row<T, D>(a, u.seq, u.h, query_of<T, D>(a, u, r), k0, k1, lane, m, l, o);
                 if (lane < TW) { s_m[lane][r] = lane == 0 ? m : -__builtin_inff(); s_l[lane][r] = lane == 0 ? l : 0.f; }
 #pragma unroll
                 for (int e = 0; e < D / 64; ++e) {
@@ -426,7 +426,7 @@ paged_rows_kernel(PagedArgs<T> a, PagedScratch sc, int least, int row_lo, int ro
         }
         auto finish = [&](int r, int p, const PieceSum& s) {
             const float inv = inverse(s.l);
-            const int64_t at = result_of(a, u, u.row0 + r);
+            const int64_t at = result_of(a, u, r);
             store_out4(a.out + at * D + 4 * p, f32x4{s.o[0] * inv, s.o[1] * inv, s.o[2] * inv, s.o[3] * inv});
             if (a.lse && p == 0) a.lse[at] = natural_lse(s.m, s.l);
         };

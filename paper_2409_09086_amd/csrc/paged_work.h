@@ -27,7 +27,18 @@ struct Unit {
     int kb, ke;        // keys that any of its rows sees
     int r0, r1;        // the team's runs of RUN keys of it, counted from align(kb)
     int pieces, piece, team0;   // the teams that share it: team0 + 0 .. pieces - 1; this is number `piece`
-    __device__ __forceinline__ int pos(int row) const { return pos0 + row / G; }
+    int tok0, rem0;    // row0 = tok0 * G + rem0
+    uint32_t inv_g;
+    // Token of the unit's row r and its head in the group.  x * inv_g / 2^32 exceeds x / G by less than x / 2^32, so it is exact for
+    // x < R + G, G * (R + G) < 2^32.
+    __device__ __forceinline__ int token(int r, int& head) const
+    {
+        const int x = rem0 + r, t = G == 1 ? x : (int)__umulhi((uint32_t)x, inv_g);
+        head = x - t * G;
+        return tok0 + t;
+    }
+    __device__ __forceinline__ int token(int r) const { int head; return token(r, head); }
+    __device__ __forceinline__ int pos(int r) const { return pos0 + token(r); }
 };
 
 // R rows a unit; keys in runs of RUN from a multiple of RUN.
@@ -35,6 +46,7 @@ template <int R, int RUN>
 struct Work {
     const int32_t *starts, *lens;
     int seqs, tokens, G, Hkv, window, row_lo, row_hi, team, teams;
+    uint32_t inv_g;
     int most_keys;             // what a sequence's row of the page table holds
     double chunk, left, off, u0;   // of a share; left of mine; where in the unit I am; where the unit starts
     int seq, h, tile;
@@ -70,7 +82,7 @@ struct Work {
     template <typename T>
     __device__ __forceinline__ Work(const PagedArgs<T>& a, int team_, int teams_, int least, int row_lo_, int row_hi_, int lane)
         : starts(a.starts), lens(a.lens), seqs(a.seqs), tokens(a.tokens), G(a.G), Hkv(a.Hkv), window(a.window), row_lo(row_lo_),
-          row_hi(row_hi_), team(team_), teams(teams_)
+          row_hi(row_hi_), team(team_), teams(teams_), inv_g(a.inv_g)
     {
         most_keys = (int)min((int64_t)a.pages_per_seq << a.page_shift, (int64_t)INT32_MAX - 65536);
         const int per = (seqs + 63) / 64;                      // consecutive sequences of a lane
@@ -135,9 +147,11 @@ struct Work {
         if (!(left > 0.0)) return false;
         const double cost = base + (tile + 1) * inc, take_ = fmin(cost - off, left), end = off + take_;
         u.first = first; u.G = G; u.rows = n * G; u.pos0 = pos0; u.seq = seq; u.h = h; u.row0 = tile * R;
-        const int last = min(u.row0 + R, u.rows) - 1;
-        u.ke = min(max(u.pos(last) + 1, 0), most_keys);
-        u.kb = window > 0 ? min(max(u.pos(u.row0) + 1 - window, 0), u.ke) : 0;
+        u.tok0 = __builtin_amdgcn_readfirstlane(u.row0 / G);
+        u.rem0 = __builtin_amdgcn_readfirstlane(u.row0 - u.tok0 * G);
+        u.inv_g = inv_g;
+        u.ke = min(max(u.pos(min(R, u.rows - u.row0) - 1) + 1, 0), most_keys);
+        u.kb = window > 0 ? min(max(u.pos(0) + 1 - window, 0), u.ke) : 0;
         const int runs = (u.ke - (u.kb & ~(RUN - 1)) + RUN - 1) / RUN;
         u.r0 = 0; u.r1 = runs; u.pieces = 1; u.piece = 0; u.team0 = team;
         if (off > 0.0 || end < cost) {

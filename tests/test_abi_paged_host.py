@@ -25,7 +25,8 @@ def test_rotary_create_refuses(args):
 
 
 @pytest.mark.parametrize("args", [dict(pages=0), dict(pages=(1 << 30) + 1), dict(page=8), dict(page=24), dict(page=2048), dict(heads=3), dict(heads=0),
-                                  dict(kv=0), dict(kv=-2), dict(d=96), dict(dtype=2), dict(heads=1 << 17)])
+                                  dict(kv=0), dict(kv=-2), dict(d=96), dict(dtype=2), dict(heads=1 << 17),
+                                  dict(heads=8192, kv=1), dict(heads=65536, kv=65536, page=1024, d=128)])
 def test_paged_create_refuses(args):
     rc, h = paged(**args)
     assert rc == B.EINVAL and not h.value and B.last_error()

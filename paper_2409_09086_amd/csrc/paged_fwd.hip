@@ -102,7 +102,10 @@ paged_fwd_kernel(PagedArgs<uint16_t> a, PagedScratch sc, int least, int row_lo, 
     constexpr int NS = D / 16, NB = D / 32, SLOTS = D / 8, PER = 32 / SLOTS;   // products along D, column blocks; slots of half a period, logits of a slot
     constexpr int VECS = PF_VECS<D>, SLOT = PF_SLOT<D>;
     static_assert(NBUF * TBYTES <= 65536, "a region must be addressable with a 16-bit instruction offset");
-    typedef Work<PF_ROWS, PF_TILE> W;
+    // What a unit costs beside its keys (queries, first tiles, output), in keys: us with 64 / 128 / 256 / 384 / 768, 4096 tokens on themselves, 32
+    // heads on 8: 201.9 / 183.9 / 161.2 / 152.3 / 153.6; four chunks of 300..700 over up to 3000 keys 108.9 / 105.9 / 103.2 / 102.9 / 101.0.
+    constexpr int OVERHEAD = 384;
+    typedef Work<PF_ROWS, PF_TILE, OVERHEAD> W;
     constexpr int WORK = (sizeof(W) + 15) / 16 * 16;
     __shared__ __attribute__((aligned(1024))) char smem[DUMP + 4 * 1024];
     __shared__ __attribute__((aligned(16))) char s_work[4][WORK];
@@ -511,54 +514,80 @@ paged_fwd_kernel(PagedArgs<uint16_t> a, PagedScratch sc, int least, int row_lo, 
                     }
                 }
             }
-        } else if (u.pieces > 1) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int q4 = 0; q4 < 4; ++q4)
-                        __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(o[x][b][4 * q4]), __float_as_uint(o[x][b][4 * q4 + 1]),
-                                                                     __float_as_uint(o[x][b][4 * q4 + 2]), __float_as_uint(o[x][b][4 * q4 + 3])},
-                                                               own, el * 16, part_off + (4 * NB * x + 4 * b + q4) * 1024, SC1);
-            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(m_ref[0]), __float_as_uint(ltot[0]),
-                                                         __float_as_uint(m_ref[1]), __float_as_uint(ltot[1])},
-                                                   own, el * 16, part_off + (VECS - 1) * 1024, SC1);
         }
-        bool mine = u.pieces == 1;                             // whether this workgroup stores the unit's results from its registers
+        bool mine = true;                                      // whether this workgroup stores the unit's results
         if (u.pieces > 1) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (threadIdx.x == 0) s_flag[4] = __hip_atomic_fetch_add(sc.arrived + u.team0, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __syncthreads();
-            mine = __builtin_amdgcn_readfirstlane(s_flag[4]) == u.pieces - 1;
-            if (mine) {                                        // the last to arrive merges, in the pieces' order
-                if (threadIdx.x == 0) __hip_atomic_store(sc.arrived + u.team0, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
-#pragma nounroll
-                for (int i = 0; i < (active ? u.pieces : 0); ++i) {
-                    const auto src = slot_rsrc(sc.part, 2 * (u.team0 + i) + (i == 0), SLOT);
-                    const u32x4 ml = __builtin_amdgcn_raw_buffer_load_b128(src, el * 16, part_off + (VECS - 1) * 1024, SC1);
+            auto leave = [&]() {
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        u32x4 other[4 * NB];
+                for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int v = 0; v < 4 * NB; ++v)
-                            other[v] = __builtin_amdgcn_raw_buffer_load_b128(src, el * 16, part_off + (4 * NB * x + v) * 1024, SC1);
-                        const float mo = __uint_as_float(ml[2 * x]), lo_ = __uint_as_float(ml[2 * x + 1]);
-                        if (i == 0) { m_ref[x] = -__builtin_inff(); ltot[x] = 0.f; }
-                        const float mt = fmaxf(m_ref[x], mo), mz = mt == -__builtin_inff() ? 0.f : mt;
-                        const float w = fast_exp2(m_ref[x] - mz), wo = fast_exp2(mo - mz);
-                        m_ref[x] = mt;
-                        ltot[x] = __builtin_fmaf(w, ltot[x], wo * lo_);
+                    for (int b = 0; b < NB; ++b)
 #pragma unroll
-                        for (int v = 0; v < 4 * NB; ++v)
+                        for (int q4 = 0; q4 < 4; ++q4)
+                            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(o[x][b][4 * q4]), __float_as_uint(o[x][b][4 * q4 + 1]),
+                                                                         __float_as_uint(o[x][b][4 * q4 + 2]), __float_as_uint(o[x][b][4 * q4 + 3])},
+                                                                   own, el * 16, part_off + (4 * NB * x + 4 * b + q4) * 1024, SC1);
+                __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(m_ref[0]), __float_as_uint(ltot[0]),
+                                                             __float_as_uint(m_ref[1]), __float_as_uint(ltot[1])},
+                                                       own, el * 16, part_off + (VECS - 1) * 1024, SC1);
+            };
+            // o, m, l = fa (o, m, l) + fb (those of a slot); products rounded before they are added: the same bits whichever of two pieces does it
+            auto add = [&](int slot, bool first) {
+#pragma clang fp contract(off)
+                const auto src = slot_rsrc(sc.part, slot, SLOT);
+                const u32x4 ml = __builtin_amdgcn_raw_buffer_load_b128(src, el * 16, part_off + (VECS - 1) * 1024, SC1);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float acc = i == 0 ? 0.f : o[x][v >> 2][4 * (v & 3) + e];
-                                o[x][v >> 2][4 * (v & 3) + e] = __builtin_fmaf(w, acc, wo * __uint_as_float(other[v][e]));
-                            }
+                for (int x = 0; x < 2; ++x) {
+                    u32x4 other[4 * NB];
+#pragma unroll
+                    for (int v = 0; v < 4 * NB; ++v)
+                        other[v] = __builtin_amdgcn_raw_buffer_load_b128(src, el * 16, part_off + (4 * NB * x + v) * 1024, SC1);
+                    const float mo = __uint_as_float(ml[2 * x]), lo_ = __uint_as_float(ml[2 * x + 1]);
+                    if (first) {
+                        m_ref[x] = mo;
+                        ltot[x] = lo_;
                     }
+                    const float mt = fmaxf(m_ref[x], mo), mz = mt == -__builtin_inff() ? 0.f : mt;
+                    const float w = fast_exp2(m_ref[x] - mz), wo = fast_exp2(mo - mz);   // no key seen: m = -inf, weight 0
+                    m_ref[x] = mt;
+                    if (!first) ltot[x] = w * ltot[x] + wo * lo_;
+#pragma unroll
+                    for (int v = 0; v < 4 * NB; ++v)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float y = __uint_as_float(other[v][e]);
+                            o[x][v >> 2][4 * (v & 3) + e] = first ? y : w * o[x][v >> 2][4 * (v & 3) + e] + wo * y;
+                        }
                 }
+            };
+            if (__builtin_expect(again, 0)) {                  // what plain_row left
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                add(W::slot(u, u.piece), true);
+            }
+            // Pieces are merged pairwise, a binary tree over their numbers: the first of two halves to come to a node leaves its sum in its
+            // slot and its name at the node, the second adds that to its own and goes on.  (One workgroup that merged all of them took
+            // 3 us a piece: 140 us for 64 tokens of 32 heads on 8 over 30000 keys, in 32 pieces each; so 79.)
+#pragma nounroll
+            for (int width = 1; width < u.pieces; width *= 2) {
+                const int mid = (u.piece & ~(2 * width - 1)) + width;   // the first piece of the node's upper half
+                if (mid >= u.pieces) continue;                 // there is none
+                int* const node = sc.arrived + u.team0 + mid;  // no other unit has this team for a piece but its first
+                __syncthreads();
+                if (threadIdx.x == 0) s_flag[4] = __hip_atomic_load(node, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __syncthreads();
+                int other = __builtin_amdgcn_readfirstlane(s_flag[4]);
+                if (other == 0) {
+                    leave();
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    __syncthreads();
+                    if (threadIdx.x == 0) s_flag[4] = __hip_atomic_exchange(node, team + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __syncthreads();
+                    other = __builtin_amdgcn_readfirstlane(s_flag[4]);
+                    if (other == 0) { mine = false; break; }   // the other half will find it
+                }
+                if (threadIdx.x == 0) __hip_atomic_store(node, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
+                add(W::slot(u, other - 1 - u.team0), false);
             }
         }
         if (mine && active && !(again && u.pieces == 1)) {

@@ -374,8 +374,11 @@ paged_rows_kernel(PagedArgs<T> a, PagedScratch sc, int least, int row_lo, int ro
     // 16-byte piece p of row r of wavefront w's share lies in slot p ^ ((r ^ w) & 7) of the row
     auto share = [&](int w, int r, int p) -> f32x4* { return (f32x4*)(smem + w * STAGE + r * (D * 4) + ((p ^ ((r ^ w) & 7)) * 16)); };
 
-    // a wavefront's place in its share: in LDS, the loop over the keys wants the registers
-    typedef Work<ROWS, KEYS> W;
+    // a wavefront's place in its share is in LDS, the loop over the keys wants the registers
+    // What a unit costs beside its keys, in keys: us with 16 / 64 / 128 / 256, 64 tokens over 256..8192 keys of 8 kv-heads 205.7 / 202.3 / 198.7 /
+    // 196.9, 16 over 2000..6000 61.9 / 54.2 / 54.5 / 53.7, 512 over 10..300 90.3 / 80.8 / 80.7 / 81.5.
+    constexpr int OVERHEAD = 128;
+    typedef Work<ROWS, KEYS, OVERHEAD> W;
     __shared__ __attribute__((aligned(16))) char s_work[TW][(sizeof(W) + 15) / 16 * 16];
     W* const place = (W*)s_work[wave];
     *place = W(a, blockIdx.x, gridDim.x, least, row_lo, row_hi, lane);

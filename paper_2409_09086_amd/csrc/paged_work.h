@@ -4,11 +4,11 @@
 // that a group's heads share every key.  Nothing about the sequences is known on the host.  Every team (a workgroup or a
 // wavefront) therefore reads the batch's arrays itself, adds up what all units cost and takes its share of the whole, from
 // where the shares of the teams before it end: the chip is filled evenly whatever the lengths are, a long sequence is cut over
-// many teams, and a team has at most two units that others work on too, its first and its last.  Those leave
-// their partial results (un-normalised output, reference, sum) in the team's two slots, and the team that arrives last merges
-// the unit's pieces in their order, so that results do not depend on who that is.
+// many teams, and a team has at most two units that others work on too, its first and its last.  Partial results of those
+// (un-normalised output, reference, sum) go through the team's two slots, and are added in an order that does not depend on who does
+// it; no team waits for another one.
 //
-// A unit costs its keys and OVERHEAD keys for queries and output, in whole numbers far below 2^53, held in doubles (64-bit
+// A unit costs its keys and OVERHEAD keys for everything else, in whole numbers far below 2^53, held in doubles (64-bit
 // divisions in integers take a microsecond).  Shares are cut anywhere; the cut is rounded down to a run of keys, alike on both
 // sides of it.
 #pragma once
@@ -16,8 +16,6 @@
 
 namespace infmllm {
 namespace {
-
-constexpr int WORK_OVERHEAD = 64;
 
 struct Unit {
     int first;         // token of row 0 of the sequence
@@ -41,8 +39,8 @@ struct Unit {
     __device__ __forceinline__ int pos(int r) const { return pos0 + token(r); }
 };
 
-// R rows a unit; keys in runs of RUN from a multiple of RUN.
-template <int R, int RUN>
+// R rows a unit; keys in runs of RUN from a multiple of RUN; a unit costs OVERHEAD keys more than it has.
+template <int R, int RUN, int OVERHEAD>
 struct Work {
     const int32_t *starts, *lens;
     int seqs, tokens, G, Hkv, window, row_lo, row_hi, team, teams;
@@ -69,8 +67,8 @@ struct Work {
         q.pos0 = q.n > 0 ? len - (s1 - q.first) : 0;
         q.ntile = (int)((q.n * (int64_t)G + R - 1) / R);
         const int ctx = min(max(q.pos0, 0), most_keys), step = max(R / G, 1);
-        if (window > 0) { q.base = (double)WORK_OVERHEAD + min((double)ctx + q.n, (double)window + step); q.inc = 0.0; }
-        else { q.base = (double)WORK_OVERHEAD + ctx; q.inc = (double)step; }
+        if (window > 0) { q.base = (double)OVERHEAD + min((double)ctx + q.n, (double)window + step); q.inc = 0.0; }
+        else { q.base = (double)OVERHEAD + ctx; q.inc = (double)step; }
         return q;
     }
     static __device__ __forceinline__ double before(const Seq& q, int i) { return i * q.base + q.inc * (0.5 * i * (i + 1.0)); }

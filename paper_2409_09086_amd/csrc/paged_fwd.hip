@@ -104,7 +104,7 @@ paged_fwd_kernel(PagedArgs<uint16_t> a, PagedScratch sc, int least, int row_lo, 
     static_assert(NBUF * TBYTES <= 65536, "a region must be addressable with a 16-bit instruction offset");
     // What a unit costs beside its keys (queries, first tiles, output), in keys: us with 64 / 128 / 256 / 384 / 768, 4096 tokens on themselves, 32
     // heads on 8: 201.9 / 183.9 / 161.2 / 152.3 / 153.6; four chunks of 300..700 over up to 3000 keys 108.9 / 105.9 / 103.2 / 102.9 / 101.0.
-    constexpr int OVERHEAD = 384;
+    constexpr int OVERHEAD = 512;
     typedef Work<PF_ROWS, PF_TILE, OVERHEAD> W;
     constexpr int WORK = (sizeof(W) + 15) / 16 * 16;
     __shared__ __attribute__((aligned(1024))) char smem[DUMP + 4 * 1024];

@@ -377,7 +377,7 @@ paged_rows_kernel(PagedArgs<T> a, PagedScratch sc, int least, int row_lo, int ro
     // a wavefront's place in its share is in LDS, the loop over the keys wants the registers
     // What a unit costs beside its keys, in keys: us with 16 / 64 / 128 / 256, 64 tokens over 256..8192 keys of 8 kv-heads 205.7 / 202.3 / 198.7 /
     // 196.9, 16 over 2000..6000 61.9 / 54.2 / 54.5 / 53.7, 512 over 10..300 90.3 / 80.8 / 80.7 / 81.5.
-    constexpr int OVERHEAD = 128;
+    constexpr int OVERHEAD = TW == 1 ? 32 : 192;
     typedef Work<ROWS, KEYS, OVERHEAD> W;
     __shared__ __attribute__((aligned(16))) char s_work[TW][(sizeof(W) + 15) / 16 * 16];
     W* const place = (W*)s_work[wave];

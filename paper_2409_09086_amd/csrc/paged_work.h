@@ -8,9 +8,9 @@
 // (un-normalised output, reference, sum) go through the team's two slots, and are added in an order that does not depend on who does
 // it; no team waits for another one.
 //
-// A unit costs its keys and OVERHEAD keys for everything else, in whole numbers far below 2^53, held in doubles (64-bit
-// divisions in integers take a microsecond).  Shares are cut anywhere; the cut is rounded down to a run of keys, alike on both
-// sides of it.
+// A unit costs OVERHEAD keys for everything but its keys, ahead of them, and its keys, in whole numbers far below 2^53, held in
+// doubles (64-bit divisions in integers take a microsecond).  A share that begins in a unit's overhead has the unit's first keys, one
+// that ends there has none of it; among the keys a share ends anywhere, rounded down to a run, alike on both sides.
 #pragma once
 #include "paged.h"
 
@@ -144,6 +144,7 @@ struct Work {
     {
         if (!(left > 0.0)) return false;
         const double cost = base + (tile + 1) * inc, take_ = fmin(cost - off, left), end = off + take_;
+        if (end < cost && end <= OVERHEAD) return false;       // my share ends ahead of its first key
         u.first = first; u.G = G; u.rows = n * G; u.pos0 = pos0; u.seq = seq; u.h = h; u.row0 = tile * R;
         u.tok0 = __builtin_amdgcn_readfirstlane(u.row0 / G);
         u.rem0 = __builtin_amdgcn_readfirstlane(u.row0 - u.tok0 * G);
@@ -152,10 +153,11 @@ struct Work {
         u.kb = window > 0 ? min(max(u.pos(0) + 1 - window, 0), u.ke) : 0;
         const int runs = (u.ke - (u.kb & ~(RUN - 1)) + RUN - 1) / RUN;
         u.r0 = 0; u.r1 = runs; u.pieces = 1; u.piece = 0; u.team0 = team;
-        if (off > 0.0 || end < cost) {
-            if (off > 0.0) u.r0 = (int)(runs * off / cost);
-            if (end < cost) u.r1 = (int)(runs * end / cost);
-            u.team0 = min(max((int)(u0 / chunk), 0), team);
+        if (off > OVERHEAD || end < cost) {
+            const double per_cost = runs / (cost - OVERHEAD);
+            if (off > OVERHEAD) u.r0 = min((int)((off - OVERHEAD) * per_cost), runs);
+            if (end < cost) u.r1 = min((int)((end - OVERHEAD) * per_cost), runs);
+            u.team0 = min(max((int)((u0 + OVERHEAD) / chunk), 0), team);
             u.pieces = min((int)((u0 + cost - 1.0) / chunk), teams - 1) - u.team0 + 1;
             u.piece = team - u.team0;
         }

@@ -346,9 +346,14 @@ def _rows(t, dtype, tokens, heads, head_dim, name):
     return t.data_ptr(), s0 if tokens > 1 else max(s0, heads * head_dim)
 
 
+def _pool(t, dtype, shape, name):
+    """Address of a dense tensor (as _dev_ptr, without its objects: the calls below are short)."""
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous device tensor of shape %s and dtype %s" % (name, tuple(shape), dtype))
+    return t.data_ptr()
+
+
 def _weight(w, dtype, head_dim, name):
-    if w is None:
-        return None
     if not w.is_cuda or w.dtype != dtype or w.shape != (head_dim,) or not w.is_contiguous():
         raise ValueError("%s must be a contiguous device tensor of %d elements of dtype %s" % (name, head_dim, dtype))
     return w.data_ptr()
@@ -403,26 +408,26 @@ class Rotary(_Attached):
         """infmllm_rotary_apply: q [n, heads, d], k [n, kv_heads, d] (either may be None), positions int32 [n].
         Returns (q_out, k_out); q_out=q turns in place.  Nothing is synchronised."""
         n, d, dt = positions.shape[0], self.head_dim, self.dtype
-        _dev_ptr(positions, torch.int32, (n,), "positions")
-        args = []
-        heads = []
-        outs = []
-        for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
-            if x is None:
-                heads.append(0)
-                args.append((None, 0, None, 0))
-                outs.append(None)
-                continue
-            hx = x.shape[1]
-            if out is None:
-                out = torch.empty((n, hx, d), dtype=dt, device=x.device)
-            heads.append(hx)
-            args.append(_rows(x, dt, n, hx, d, name) + (_rows(out, dt, n, hx, d, name + "_out")))
-            outs.append(out)
-        (qp, qs, qo, qos), (kp, ks, ko, kos) = args
-        _check(lib().infmllm_rotary_apply(self._h, positions.data_ptr(), n, heads[0], heads[1], qp, qs, kp, ks,
-                                          _weight(q_weight, dt, d, "q_weight"), _weight(k_weight, dt, d, "k_weight"), qo, qos, ko, kos))
-        return outs[0], outs[1]
+        if positions.dtype != torch.int32 or positions.dim() != 1 or not positions.is_cuda or not positions.is_contiguous():
+            raise ValueError("positions must be a contiguous device tensor of int32 [n]")
+        heads = kv_heads = qs = ks = qos = kos = 0
+        qp = kp = qo = ko = None
+        if q is not None:
+            heads = q.shape[1]
+            if q_out is None:
+                q_out = torch.empty_like(q)
+            qp, qs = _rows(q, dt, n, heads, d, "q")
+            qo, qos = _rows(q_out, dt, n, heads, d, "q_out")
+        if k is not None:
+            kv_heads = k.shape[1]
+            if k_out is None:
+                k_out = torch.empty_like(k)
+            kp, ks = _rows(k, dt, n, kv_heads, d, "k")
+            ko, kos = _rows(k_out, dt, n, kv_heads, d, "k_out")
+        _check(_lib.infmllm_rotary_apply(self._h, positions.data_ptr(), n, heads, kv_heads, qp, qs, kp, ks,
+                                         None if q_weight is None else _weight(q_weight, dt, d, "q_weight"),
+                                         None if k_weight is None else _weight(k_weight, dt, d, "k_weight"), qo, qos, ko, kos))
+        return (None if q is None else q_out), (None if k is None else k_out)
 
 
 class _Batch(ctypes.Structure):
@@ -472,15 +477,19 @@ class PagedCache(_Attached):
         """infmllm_paged_append: k, v [tokens, kv_heads, d] enter the pools K, V; with a Rotary, keys and (where given) queries q
         [tokens, heads, d] are normed and turned on the way.  Returns q_out (None without q).  Nothing is synchronised."""
         n, d, dt = batch.tokens, self.head_dim, self.dtype
-        qp = qs = qo = qos = None
+        qs = qos = 0
+        qp = qo = None
         if q is not None:
             if q_out is None:
-                q_out = torch.empty((n, self.heads, d), dtype=dt, device=q.device)
-            (qp, qs), (qo, qos) = _rows(q, dt, n, self.heads, d, "q"), _rows(q_out, dt, n, self.heads, d, "q_out")
-        (kp, ks), (vp, vs) = _rows(k, dt, n, self.kv_heads, d, "k"), _rows(v, dt, n, self.kv_heads, d, "v")
-        _check(lib().infmllm_paged_append(self._h, None if rotary is None else rotary._h, batch._ref, kp, ks, vp, vs,
-                                          _weight(k_weight, dt, d, "k_weight"), qp, qs or 0, _weight(q_weight, dt, d, "q_weight"), qo, qos or 0,
-                                          _dev_ptr(K, dt, self.pool_shape, "K"), _dev_ptr(V, dt, self.pool_shape, "V")))
+                q_out = torch.empty_like(q)
+            qp, qs = _rows(q, dt, n, self.heads, d, "q")
+            qo, qos = _rows(q_out, dt, n, self.heads, d, "q_out")
+        kp, ks = _rows(k, dt, n, self.kv_heads, d, "k")
+        vp, vs = _rows(v, dt, n, self.kv_heads, d, "v")
+        _check(_lib.infmllm_paged_append(self._h, None if rotary is None else rotary._h, batch._ref, kp, ks, vp, vs,
+                                         None if k_weight is None else _weight(k_weight, dt, d, "k_weight"), qp, qs,
+                                         None if q_weight is None else _weight(q_weight, dt, d, "q_weight"), qo, qos,
+                                         _pool(K, dt, self.pool_shape, "K"), _pool(V, dt, self.pool_shape, "V")))
         return q_out if q is not None else None
 
     def attend(self, batch, q, K, V, out=None, lse=None):
@@ -490,7 +499,7 @@ class PagedCache(_Attached):
         qp, qs = _rows(q, dt, n, self.heads, d, "q")
         if out is None:
             out = torch.empty((n, self.heads, d), dtype=dt, device=q.device)
-        _check(lib().infmllm_paged_attend(self._h, batch._ref, qp, qs, _dev_ptr(K, dt, self.pool_shape, "K"),
-                                          _dev_ptr(V, dt, self.pool_shape, "V"), _dev_ptr(out, dt, (n, self.heads, d), "out"),
-                                          _dev_ptr(lse, torch.float32, (n, self.heads), "lse")))
+        _check(_lib.infmllm_paged_attend(self._h, batch._ref, qp, qs, _pool(K, dt, self.pool_shape, "K"), _pool(V, dt, self.pool_shape, "V"),
+                                         _pool(out, dt, (n, self.heads, d), "out"),
+                                         None if lse is None else _pool(lse, torch.float32, (n, self.heads), "lse")))
         return out

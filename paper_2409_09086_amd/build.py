@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libinfmllm.so")
 SOURCES = ["api.hip", "cache_kernels.hip", "attn_simple.hip", "attn_f32.hip", "attn_mfma.hip", "attn_mfma64.hip", "attn_rows.hip", "attn_rows64.hip", "decode_attn.hip", "rope.hip", "select_kernel.hip",
-           "rotary.hip", "paged_rows.hip", "paged_fwd.hip", "paged_api.hip"]
+           "rotary.hip", "paged_rows.hip", "paged_fwd.hip", "paged_mixed.hip", "paged_api.hip"]
 # packed-fp32 instructions are switched off for every device pass
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

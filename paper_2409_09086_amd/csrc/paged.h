@@ -40,17 +40,20 @@ struct PagedArgs {
     uint32_t inv_g;                                // 2^32 / G + 1, rounded down (G > 1): see Unit::token
     float c;                                       // scale * log2(e)
 };
-// Partial results of units that several teams share (paged_work.h): two slots a team, and a ticket for each, zero between launches.
+// Partial results of units that several teams share (paged_work.h): two slots a team, and 2 * PAGED_TEAMS tickets, zero between launches.
 struct PagedScratch { float* part; int* arrived; };
 constexpr int PAGED_CUS = 256;                     // compute units: teams of a launch with one a CU
 constexpr int PAGED_TEAMS = 8 * PAGED_CUS;         // most teams of a launch
 
-// The sequences with row_lo < new tokens * G <= row_hi; max_new: the caller's bound.
+// Few rows a unit: 16 or 32; max_new: the caller's bound.
 template <typename T>
-hipError_t launch_paged_rows(const PagedArgs<T>& a, const PagedScratch& sc, int head_dim, int max_new, int row_lo, int row_hi, hipStream_t st);
+hipError_t launch_paged_rows(const PagedArgs<T>& a, const PagedScratch& sc, int head_dim, int max_new, hipStream_t st);
 size_t paged_rows_scratch(int head_dim, int elt);  // bytes of PagedScratch::part
 // The same for bf16 chunks of many rows, 256 a unit.
-hipError_t launch_paged_fwd(const PagedArgs<uint16_t>& a, const PagedScratch& sc, int head_dim, int row_lo, int row_hi, hipStream_t st);
+hipError_t launch_paged_fwd(const PagedArgs<uint16_t>& a, const PagedScratch& sc, int head_dim, hipStream_t st);
 size_t paged_fwd_scratch(int head_dim);
+// Both in one launch: the sequences of at most `few` rows (16), and the others.
+hipError_t launch_paged_mixed(const PagedArgs<uint16_t>& a, const PagedScratch& sc, int head_dim, int few, hipStream_t st);
+size_t paged_mixed_scratch(int head_dim);
 
 }  // namespace infmllm

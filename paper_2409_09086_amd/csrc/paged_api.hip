@@ -99,8 +99,8 @@ struct infmllm_paged {
 
     int elt() const { return dtype == INFMLLM_BF16 ? 2 : 4; }
     PagedScratch sc{nullptr, nullptr};
-    size_t part_bytes() const { return up(std::max(paged_rows_scratch(d, elt()), dtype == INFMLLM_BF16 ? paged_fwd_scratch(d) : 0)); }
-    size_t bytes() const { return up(PAGED_TEAMS * sizeof(int)) + part_bytes(); }
+    size_t part_bytes() const { return up(std::max(paged_rows_scratch(d, elt()), dtype == INFMLLM_BF16 ? paged_mixed_scratch(d) : 0)); }
+    size_t bytes() const { return up(2 * PAGED_TEAMS * sizeof(int)) + part_bytes(); }
 };
 
 extern "C" {
@@ -370,16 +370,14 @@ int infmllm_paged_attend(infmllm_paged_t* p, const infmllm_batch_t* batch, const
         a.inv_g = (uint32_t)((1ull << 32) / (unsigned)a.G + 1);
         a.c = (float)(p->scale * 1.4426950408889634);
         if constexpr (sizeof(T) == 2) {
-            // Chunks of more than a few rows run 256 rows a unit; sequences beside them whose rows are one block of 16 run on their own.
+            // Chunks of more than a few rows run 256 rows a unit; beside them sequences whose rows are one block of 16 run on their own.
             const int new_max = std::min(batch->max_new, batch->tokens), few = 16;
             if ((int64_t)new_max * a.G > 2 * few) {
                 const bool alike = a.seqs == 1 || (int64_t)new_max * a.seqs == a.tokens;
-                hipError_t e = hipSuccess;
-                if (!alike) e = launch_paged_rows<T>(a, p->sc, p->d, 1, 0, few, p->st);
-                return e != hipSuccess ? e : launch_paged_fwd(a, p->sc, p->d, alike ? 0 : few, INT_MAX, p->st);
+                return alike ? launch_paged_fwd(a, p->sc, p->d, p->st) : launch_paged_mixed(a, p->sc, p->d, few, p->st);
             }
         }
-        return launch_paged_rows<T>(a, p->sc, p->d, batch->max_new, 0, INT_MAX, p->st);
+        return launch_paged_rows<T>(a, p->sc, p->d, batch->max_new, p->st);
     };
     const hipError_t e = elt == 2 ? go((uint16_t*)nullptr) : go((float*)nullptr);
     return e == hipSuccess ? INFMLLM_OK : fail_hip(e, who);

@@ -39,10 +39,18 @@ struct Unit {
     __device__ __forceinline__ int pos(int r) const { return pos0 + token(r); }
 };
 
-// R rows a unit; keys in runs of RUN from a multiple of RUN; a unit costs OVERHEAD keys more than it has.
+// Sequences sq0 .. sq0 + 63 as the batch's arrays describe them, in LDS: a wavefront's own.
+struct SeqWindow {
+    int sq0;
+    int s0[64], s1[64], len[64];
+};
+
+// R rows a unit; keys in runs of RUN from a multiple of RUN; a unit costs OVERHEAD keys more than it has.  row_lo, row_hi: the
+// sequences with row_lo < rows <= row_hi.  All lanes of a wavefront call everything here.
 template <int R, int RUN, int OVERHEAD>
 struct Work {
     const int32_t *starts, *lens;
+    SeqWindow* win;
     int seqs, tokens, G, Hkv, window, row_lo, row_hi, team, teams;
     uint32_t inv_g;
     int most_keys;             // what a sequence's row of the page table holds
@@ -52,14 +60,10 @@ struct Work {
     double base, inc;              // tile i of it costs base + (i + 1) * inc
 
     struct Seq { int first, n, pos0, ntile; double base, inc; };
-    __device__ __forceinline__ Seq load(int s) const
-    {
-        const int s0 = starts[s], s1 = starts[s + 1], len = max(lens[s], 0);
-        return describe(s0, s1, len);
-    }
     __device__ __forceinline__ Seq describe(int s0, int s1, int len) const
     {
         Seq q;
+        len = max(len, 0);
         q.first = min(max(s0, 0), tokens);
         q.n = max(min(s1, tokens) - q.first, 0);
         const int64_t rows = (int64_t)q.n * G;
@@ -71,53 +75,102 @@ struct Work {
         else { q.base = (double)OVERHEAD + ctx; q.inc = (double)step; }
         return q;
     }
+    // sequences s .. s + 63 come into the window; returns this lane's
+    __device__ __forceinline__ Seq fill(int s, int lane)
+    {
+        const int mine = min(s + lane, seqs - 1);
+        const int s0 = starts[mine], s1 = starts[mine + 1], len = lens[mine];
+        win->sq0 = s;
+        win->s0[lane] = s0; win->s1[lane] = s1; win->len[lane] = len;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        Seq q = describe(s0, s1, len);
+        if (s + lane >= seqs) q.n = 0;
+        return q;
+    }
+    __device__ __forceinline__ Seq from_window(int s) const
+    {
+        const int i = s - win->sq0;
+        return describe(__builtin_amdgcn_readfirstlane(win->s0[i]), __builtin_amdgcn_readfirstlane(win->s1[i]),
+                        __builtin_amdgcn_readfirstlane(win->len[i]));
+    }
     static __device__ __forceinline__ double before(const Seq& q, int i) { return i * q.base + q.inc * (0.5 * i * (i + 1.0)); }
     __device__ __forceinline__ double of_head(const Seq& q) const { return q.n > 0 ? before(q, q.ntile) : 0.0; }
     __device__ __forceinline__ void take(const Seq& q) { first = q.first; n = q.n; pos0 = q.pos0; ntile = q.ntile; base = q.base; inc = q.inc; }
 
-    __device__ Work() = default;
-    // All lanes of the wavefront call this.  teams: how many share the work; least: the smallest share, in keys.
-    template <typename T>
-    __device__ __forceinline__ Work(const PagedArgs<T>& a, int team_, int teams_, int least, int row_lo_, int row_hi_, int lane)
-        : starts(a.starts), lens(a.lens), seqs(a.seqs), tokens(a.tokens), G(a.G), Hkv(a.Hkv), window(a.window), row_lo(row_lo_),
-          row_hi(row_hi_), team(team_), teams(teams_), inv_g(a.inv_g)
+    static __device__ __forceinline__ double uniform(double x)
     {
-        most_keys = (int)min((int64_t)a.pages_per_seq << a.page_shift, (int64_t)INT32_MAX - 65536);
-        const int per = (seqs + 63) / 64;                      // consecutive sequences of a lane
-        double mine = 0.0;
-        Seq q{};
-        for (int i = 0; i < per; ++i) {
-            const int s = lane * per + i;
-            if (s < seqs) { q = load(s); mine += of_head(q) * Hkv; }
-        }
-        double incl = mine;
+        const uint64_t u = __builtin_bit_cast(uint64_t, x);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    }
+    static __device__ __forceinline__ double scan(double mine, int lane)       // over the lanes up to this one
+    {
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const double x = __shfl_up(incl, d);
-            if (lane >= d) incl += x;
+            const double x = __shfl_up(mine, d);
+            if (lane >= d) mine += x;
         }
-        const double total = uniform(__shfl(incl, 63));
-        chunk = fmax(ceil(total / teams), (double)least);
-        const double lo = team * chunk;
-        left = fmin(chunk, total - lo);
-        if (!(left > 0.0)) { left = 0.0; return; }
-        const int who = __builtin_ctzll(__ballot(incl > lo));
-        double rem = lo - uniform(__shfl(incl - mine, who));
-        seq = who * per;
-        Seq now;
-        for (;;) {                                             // the sequence in that lane's block
-            if (per == 1) {
-                now.first = __builtin_amdgcn_readlane(q.first, who); now.n = __builtin_amdgcn_readlane(q.n, who);
-                now.pos0 = __builtin_amdgcn_readlane(q.pos0, who); now.ntile = __builtin_amdgcn_readlane(q.ntile, who);
-                now.base = uniform(__shfl(q.base, who)); now.inc = uniform(__shfl(q.inc, who));
-                break;
+        return mine;
+    }
+
+    // Cost of a lane's sequences and those of the lanes before it, of its own, and of all.
+    struct Sums { double incl, mine, total; };
+    template <typename T>
+    __device__ __forceinline__ Sums measure(const PagedArgs<T>& a, SeqWindow* win_, int row_lo_, int row_hi_, int lane)
+    {
+        starts = a.starts; lens = a.lens; win = win_;
+        seqs = a.seqs; tokens = a.tokens; G = a.G; Hkv = a.Hkv; window = a.window; row_lo = row_lo_; row_hi = row_hi_; inv_g = a.inv_g;
+        most_keys = (int)min((int64_t)a.pages_per_seq << a.page_shift, (int64_t)INT32_MAX - 65536);
+        double mine;
+        if (seqs <= 64) {
+            mine = of_head(fill(0, lane)) * Hkv;
+        } else {                                               // a block of consecutive sequences a lane
+            const int per = (seqs + 63) / 64;
+            mine = 0.0;
+            for (int i0 = 0; i0 < per; i0 += 8) {              // loads of eight at a time
+                int s0[8], s1[8], len[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int s = min(lane * per + i0 + i, seqs - 1);
+                    s0[i] = starts[s]; s1[i] = starts[s + 1]; len[i] = lens[s];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i0 + i < per && lane * per + i0 + i < seqs) mine += of_head(describe(s0[i], s1[i], len[i])) * Hkv;
             }
-            now = load(seq);
-            const double c = of_head(now) * Hkv;
-            if (rem < c || seq + 1 >= seqs) break;
-            rem -= c;
-            ++seq;
         }
+        const double incl = scan(mine, lane);
+        return Sums{incl, mine, uniform(__shfl(incl, 63))};
+    }
+    // Finds where my share begins.  least: the smallest share, in keys.
+    __device__ __forceinline__ void begin(const Sums& sums, int team_, int teams_, int least, int lane)
+    {
+        team = team_; teams = teams_;
+        chunk = fmax(ceil(sums.total / teams), (double)least);
+        const double lo = team * chunk;
+        left = fmin(chunk, sums.total - lo);
+        if (!(left > 0.0)) { left = 0.0; return; }
+        const int who = __builtin_ctzll(__ballot(sums.incl > lo));
+        double rem = lo - uniform(__shfl(sums.incl - sums.mine, who));
+        if (seqs <= 64) {
+            seq = who;
+        } else {                                               // in that lane's block
+            const int per = (seqs + 63) / 64;
+            for (int c = 0;; c += 64) {
+                const Seq q = fill(who * per + c, lane);
+                const double own = c + lane < per ? of_head(q) * Hkv : 0.0, sum = scan(own, lane), all = uniform(__shfl(sum, 63));
+                if (rem < all || c + 64 >= per) {
+                    const uint64_t past = __ballot(sum > rem);
+                    const int w = past ? __builtin_ctzll(past) : 0;
+                    rem -= uniform(__shfl(sum - own, w));
+                    seq = who * per + c + w;
+                    break;
+                }
+                rem -= all;
+            }
+        }
+        const Seq now = from_window(seq);
+        if (now.n == 0) { left = 0.0; return; }                // costs beyond 2^53 alone
         take(now);
         const double head = of_head(now);
         h = (int)(rem / head);
@@ -133,14 +186,8 @@ struct Work {
         off = uniform(rem - before(now, tile));
         u0 = lo - off;
     }
-    static __device__ __forceinline__ double uniform(double x)
-    {
-        const uint64_t u = __builtin_bit_cast(uint64_t, x);
-        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
-        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-    }
     // The next piece of my share; false: there is none.
-    __device__ __forceinline__ bool next(Unit& u)
+    __device__ __forceinline__ bool next(Unit& u, int lane)
     {
         if (!(left > 0.0)) return false;
         const double cost = base + (tile + 1) * inc, take_ = fmin(cost - off, left), end = off + take_;
@@ -173,7 +220,8 @@ struct Work {
                 h = 0;
                 do {
                     if (++seq >= seqs) { left = 0.0; break; }
-                    take(load(seq));
+                    if (seq >= win->sq0 + 64) fill(seq, lane);
+                    take(from_window(seq));
                 } while (n == 0);
             }
         }

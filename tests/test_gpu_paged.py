@@ -183,6 +183,20 @@ def test_attend(dtype, heads, kv, d, page, window, seqs):
     c.check(*other, what="wide bounds")
 
 
+@pytest.mark.parametrize("seqs,share,chunk,window", [(65, 1.0, 0, 0), (200, 0.7, 90, 0), (640, 1.0, 0, 30), (1100, 0.4, 0, 0), (5000, 0.05, 33, 0)])
+def test_many_sequences(seqs, share, chunk, window):
+    """More sequences than a wavefront has lanes, some without new tokens, perhaps a chunk among them."""
+    print("many", seqs, share, chunk, window, flush=True)
+    g = gen(seqs)
+    new = (torch.rand(seqs, generator=g) < share).long().tolist()
+    lens = [int(x) + n for x, n in zip(torch.randint(0, 90, (seqs,), generator=g), new)]
+    if chunk:
+        new[seqs // 3], lens[seqs // 3] = chunk, chunk + 200
+    c = Case(seqs, "bf16", 4, 2, 64, 16, list(zip(new, lens)), window)
+    out, lse = c.attend()
+    c.check(out, lse)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("what", ["value", "key"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])

@@ -75,9 +75,10 @@ def test_rows_kernels():
 
 
 @needs_hipcc
-def test_fwd_kernels():
-    kernels, scratch = device_code("paged_fwd.hip")
-    mine = {k: v for k, v in kernels.items() if "paged_fwd_kernel" in k}
+@pytest.mark.parametrize("name", ["paged_fwd", "paged_mixed"])
+def test_fwd_kernels(name):
+    kernels, scratch = device_code(name + ".hip")
+    mine = {k: v for k, v in kernels.items() if name + "_kernel" in k}
     assert len(mine) == 4, sorted(kernels)
     for k, body in mine.items():
         assert scratch[k] == 0, scratch
@@ -86,7 +87,7 @@ def test_fwd_kernels():
         # a V fragment's two reads fill one register quadruple, which the product reads as it stands
         reads = [int(x) for x in re.findall(r"ds_read_b64_tr_b16 v\[(\d+):\d+\]", body)]
         assert len(reads) % 2 == 0 and all(b == a + 2 for a, b in zip(reads[0::2], reads[1::2]))
-        operands = {int(x) for x in re.findall(r"v_mfma_f32_32x32x16_bf16 a\[\d+:\d+\], v\[(\d+):\d+\], v\[", body)}
+        operands = {int(x) for x in re.findall(r"v_mfma_f32_(?:32x32x16|16x16x32)_bf16 [av]\[\d+:\d+\], v\[(\d+):\d+\], v\[", body)}
         assert set(reads[0::2]) <= operands, sorted(set(reads[0::2]) - operands)
 
 

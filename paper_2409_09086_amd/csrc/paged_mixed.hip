@@ -4,9 +4,11 @@
 // matrix cores idle.  One launch gives some compute units of every XCD to the sequences of few rows (rows_body, four wavefronts with
 // two buffers each: as many bytes on their way as eight with one) and the others to the chunks (fwd_body).
 //
-// A compute unit by itself draws MIXED_CU_BYTES a microsecond, all of them together MIXED_BYTES, so that
-// decoding needs no more than some 130 units to be as fast as it gets.  Its units are then as many as make both ends finish together: where the
-// memory is the longer end, all that the chunks can do without.
+// A compute unit by itself draws MIXED_CU_BYTES a microsecond, all of them together MIXED_BYTES, so that decoding needs no more than
+// some 140 units to be as fast as it gets.  It gets as many as make both ends finish together; where the memory is the longer end,
+// all that the chunks can do without.  us, two launches one after the other / this: 512 tokens over 4206 keys beside 31 over 512..4096, 32 heads
+// on 8, 123 / 88; 2 x 256 over 1000..2000 beside 100 161 / 128; 1024 over 4500 beside 16 over 100..8000 162 / 131; 100 over 1000..2000 beside 200
+// 270 / 222; 2048 on themselves beside 60 of one key 68 / 64.  With 40e3 and 1.7 in the place of 38e3 and 2.1: 88, 153, 129, 223, 80.
 #include <algorithm>
 #include <climits>
 
@@ -16,8 +18,8 @@ namespace infmllm {
 
 namespace {
 
-constexpr double MIXED_CU_BYTES = 40e3, MIXED_BYTES = 5.3e6;   // bytes a microsecond: of a compute unit, of all
-template <int D> constexpr double MIXED_TILE_US = D == 128 ? 1.7 : 1.0;        // 256 rows by 64 keys on a compute unit
+constexpr double MIXED_CU_BYTES = 38e3, MIXED_BYTES = 5.3e6;   // bytes a microsecond: of a compute unit, of all
+template <int D> constexpr double MIXED_TILE_US = D == 128 ? 2.1 : 1.25;       // 256 rows by 64 keys on a compute unit
 constexpr int MIXED_WAVES = 4;
 
 template <int D, bool BIG>

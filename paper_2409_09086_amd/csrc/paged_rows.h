@@ -469,9 +469,9 @@ struct RowsShared {
     SeqWindow win[TW];
 };
 // What a unit costs beside its keys, in keys: us with 16 / 64 / 128 / 256, 64 tokens over 256..8192 keys of 8 kv-heads 205.7 / 202.3 / 198.7 / 196.9;
-// with 64 / 192 / 384, 256 tokens over 100..2000, a wavefront a team, 223.7 / 225.4 / 228.9.
+// with 64 / 192 / 384, 256 tokens over 100..2000, a wavefront a team, 223.7 / 225.4 / 228.9.  TW = 4: see paged_mixed.hip.
 template <typename T, int D, int NRB, int TW>
-using RowsWork = Work<16 * NRB, RowsKernel<T, D, NRB>::KEYS, TW == 1 ? 32 : 192>;
+using RowsWork = Work<16 * NRB, RowsKernel<T, D, NRB>::KEYS, TW == 1 ? 32 : TW == 4 ? 384 : 192>;
 
 // A team's share, from where sh.place says: TW wavefronts with NST buffers of a run each, at smem.
 template <typename T, int D, int NRB, int TW, int NST>

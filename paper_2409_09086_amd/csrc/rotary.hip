@@ -4,10 +4,10 @@
 // p f[i] and the row is written where it belongs: beside the input, or, for a new token's keys and values, into its page.
 // Nothing is computed twice and nothing but the rows moves, so the pass is bound by memory.
 //
-// D / 16 lanes share a row, sixteen elements each: lane c holds the elements of pairs 8c .. 8c + 7 (half-split: eight from
-// each half of the turned part, neighbouring pairs: sixteen in a row), so that a pair never leaves its lane, the norm's sum is
-// two or three lane exchanges, and a lane's eight (cos, sin) are 64 consecutive bytes of the table.  Lanes past the turned
-// part hold sixteen consecutive elements that pass.  A thread goes through HPT heads of its token, all requested before
+// D / 16 lanes share a row, two runs of eight elements each, such that a pair never leaves its lane, the norm's sum is two or three
+// lane exchanges, and the lanes' runs stand side by side in memory (sixteen elements in a row a lane, every other 16 bytes an
+// instruction, took 31.2 us for the neighbouring pairs of 4099 tokens of 64 heads of 128; so 29.5).  Half-split: the runs lie in the two halves of
+// the turned part, or of what passes behind it; neighbouring pairs: of the row, four pairs in each.  A thread goes through HPT heads of its token, all requested before
 // the first is used, with the one set of cosines.
 //
 // The table holds every position ((cos, sin) in floats, computed in doubles): 512 bytes a token beside the 20 KB that a
@@ -21,12 +21,20 @@ namespace infmllm {
 
 namespace {
 
+// PAST: past the caches, which a large pass would only sweep
+template <bool PAST>
+__device__ __forceinline__ void store16(void* p, u32x4 v)
+{
+    if constexpr (PAST) __builtin_nontemporal_store(v, (u32x4*)p);
+    else *(u32x4*)p = v;
+}
+
 // eight consecutive elements
 template <typename T> struct Eight;
 template <> struct Eight<uint16_t> {
     u32x4 raw;
     __device__ __forceinline__ void load(const uint16_t* p) { raw = *(const u32x4*)p; }
-    __device__ __forceinline__ void store(uint16_t* p) const { *(u32x4*)p = raw; }
+    template <bool PAST> __device__ __forceinline__ void store(uint16_t* p) const { store16<PAST>(p, raw); }
     __device__ __forceinline__ void get(float (&v)[8]) const
     {
 #pragma unroll
@@ -46,7 +54,11 @@ template <> struct Eight<uint16_t> {
 template <> struct Eight<float> {
     f32x4 lo, hi;
     __device__ __forceinline__ void load(const float* p) { lo = *(const f32x4*)p; hi = *(const f32x4*)(p + 4); }
-    __device__ __forceinline__ void store(float* p) const { *(f32x4*)p = lo; *(f32x4*)(p + 4) = hi; }
+    template <bool PAST> __device__ __forceinline__ void store(float* p) const
+    {
+        store16<PAST>(p, __builtin_bit_cast(u32x4, lo));
+        store16<PAST>(p + 4, __builtin_bit_cast(u32x4, hi));
+    }
     __device__ __forceinline__ void get(float (&v)[8]) const
     {
 #pragma unroll
@@ -87,11 +99,10 @@ rotary_kernel(RotaryArgs<T> a)
 
     const T* src = what == 0 ? a.q + (int64_t)tok * a.q_stride : what == 1 ? a.k + (int64_t)tok * a.k_stride : a.v + (int64_t)tok * a.v_stride;
     const T* weight = what == 0 ? a.q_weight : what == 1 ? a.k_weight : nullptr;
-    const bool turns = what < 2 && 16 * c < a.dims;
-    // the lane's two runs of eight elements
-    const bool split = a.half && turns;
-    const int ea = split ? 8 * c : 16 * c, eb = split ? a.dims / 2 + 8 * c : 16 * c + 8;
-    // lanes that pass in the half-split layout: the turned part is a multiple of 16, theirs starts behind it
+    // the lane's two runs of eight elements, and which of them are turned
+    const int part = a.half ? (16 * c < a.dims ? a.dims : D - a.dims) : D, at0 = a.half && 16 * c >= a.dims ? a.dims : 0;
+    const int ea = at0 + 8 * (a.half ? c - at0 / 16 : c), eb = ea + part / 2;
+    const bool turn_a = what < 2 && ea < a.dims, turn_b = what < 2 && eb < a.dims;
 
     Eight<T> xa[HPT], xb[HPT];
     if (exists) {
@@ -135,13 +146,15 @@ rotary_kernel(RotaryArgs<T> a)
     } else {
         dst = a.k_out + (int64_t)tok * a.k_out_stride;
     }
+    // half-split: of pairs ea .. ea + 7; neighbouring pairs: of ea / 2 .. + 3 and eb / 2 .. + 3
     float cs[8], sn[8];
-    if (turns) {
+    if (turn_a || turn_b) {
         const bool known = (unsigned)pos < (unsigned)a.max_positions;
-        const f32x4* tab = (const f32x4*)(a.table_cs + (int64_t)(known ? pos : 0) * (a.dims / 2) + 8 * c);
+        const float2* row = a.table_cs + (int64_t)(known ? pos : 0) * (a.dims / 2);
+        const f32x4 *ta = (const f32x4*)(row + (a.half ? ea : ea / 2)), *tb = a.half ? ta + 2 : (const f32x4*)(row + (turn_b ? eb / 2 : ea / 2));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const f32x4 v = tab[i];
+            const f32x4 v = i < 2 ? ta[i] : tb[i - 2];
             cs[2 * i] = v[0]; sn[2 * i] = v[1]; cs[2 * i + 1] = v[2]; sn[2 * i + 1] = v[3];
         }
         if (!known) cs[0] = cs[1] = cs[2] = cs[3] = cs[4] = cs[5] = cs[6] = cs[7] = __builtin_nanf("");
@@ -158,7 +171,7 @@ rotary_kernel(RotaryArgs<T> a)
     for (int u = 0; u < HPT; ++u) {
         if (HPT > 1 && h0 + u >= heads) break;
         Eight<T> ra = xa[u], rb = xb[u];
-        if (weight || turns) {
+        if (weight || turn_a || turn_b) {
             float x[8], y[8];
             ra.get(x);
             rb.get(y);
@@ -170,25 +183,31 @@ rotary_kernel(RotaryArgs<T> a)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) { x[e] = x[e] * r * wa[e]; y[e] = y[e] * r * wb[e]; }
             }
-            if (turns) {
-                auto turn = [&](float& p, float& q, int i) {
-                    const float p0 = p, q0 = q;
-                    p = __builtin_fmaf(p0, cs[i], -(q0 * sn[i]));
-                    q = __builtin_fmaf(q0, cs[i], p0 * sn[i]);
-                };
-                if (a.half) {
+            auto turn = [&](float& p, float& q, int i) {
+                const float p0 = p, q0 = q;
+                p = __builtin_fmaf(p0, cs[i], -(q0 * sn[i]));
+                q = __builtin_fmaf(q0, cs[i], p0 * sn[i]);
+            };
+            if (a.half) {
+                if (turn_a) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) turn(x[e], y[e], e);
-                } else {
+                }
+            } else {
+                if (turn_a) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { turn(x[2 * e], x[2 * e + 1], e); turn(y[2 * e], y[2 * e + 1], 4 + e); }
+                    for (int e = 0; e < 4; ++e) turn(x[2 * e], x[2 * e + 1], e);
+                }
+                if (turn_b) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) turn(y[2 * e], y[2 * e + 1], 4 + e);
                 }
             }
             ra.set(x);
             rb.set(y);
         }
-        ra.store(dst + (h0 + u) * hstride + ea);
-        rb.store(dst + (h0 + u) * hstride + eb);
+        ra.template store<(HPT > 1)>(dst + (h0 + u) * hstride + ea);
+        rb.template store<(HPT > 1)>(dst + (h0 + u) * hstride + eb);
     }
 }
 
@@ -212,7 +231,11 @@ hipError_t launch(const RotaryArgs<T>& a, hipStream_t st)
     const dim3 block(256);
     const unsigned gx = (unsigned)(((int64_t)a.tokens * (D / 16) + 255) / 256);
     auto groups = [&](int hpt) { return (unsigned)((a.heads + hpt - 1) / hpt + (PAGED ? 2 : 1) * ((a.kv_heads + hpt - 1) / hpt)); };
-    if ((int64_t)gx * groups(4) >= 512) hipLaunchKernelGGL((rotary_kernel<T, D, 4, PAGED>), dim3(gx, groups(4)), block, 0, st, a);
+    // Heads a thread: few tokens want threads, many want their cosines read once and their loads in a row.  us with 1 / 4 / 8 heads, the
+    // latter two with stores past the caches: 4099 tokens of 64 heads of 128 normed and turned 31.7 / 27.9 / 26.0, 8192 of 40 turned 39.2 / 33.3 / 33.8,
+    // 4236 into their pages 25.1 / 19.0 / 19.3 (22.2 with stores into the caches; the attention that follows takes as
+    // long); with 1 / 8, 2000 of 40 turned 11.2 / 10.0, 1000 (80 workgroups of 8) 9.7 / 9.7 with the call.
+    if ((int64_t)gx * groups(8) >= 256) hipLaunchKernelGGL((rotary_kernel<T, D, 8, PAGED>), dim3(gx, groups(8)), block, 0, st, a);
     else hipLaunchKernelGGL((rotary_kernel<T, D, 1, PAGED>), dim3(gx, groups(1)), block, 0, st, a);
     return hipGetLastError();
 }

@@ -9,8 +9,10 @@
 // it; no team waits for another one.
 //
 // A unit costs OVERHEAD keys for everything but its keys, ahead of them, and its keys, in whole numbers far below 2^53, held in
-// doubles (64-bit divisions in integers take a microsecond).  A share that begins in a unit's overhead has the unit's first keys, one
-// that ends there has none of it; among the keys a share ends anywhere, rounded down to a run, alike on both sides.
+// doubles (64-bit divisions in integers take a microsecond).  Shares are equal pieces of that line, but nobody works on little of a unit:
+// the team whose share ends at most HEAD into a unit leaves it to the next one, and that whose share ends at most TAIL ahead of
+// its end takes the rest along.  What a team's first unit costs beside its keys every team pays, so the unit's runs are dealt out by
+// what the shares of its teams leave for them: OVERHEAD less for a team that comes to it from another unit.
 #pragma once
 #include "paged.h"
 
@@ -49,6 +51,7 @@ struct SeqWindow {
 // sequences with row_lo < rows <= row_hi.  All lanes of a wavefront call everything here.
 template <int R, int RUN, int OVERHEAD>
 struct Work {
+    static constexpr int HEAD = OVERHEAD + 2 * RUN, TAIL = OVERHEAD / 2;
     const int32_t *starts, *lens;
     SeqWindow* win;
     int seqs, tokens, G, Hkv, window, row_lo, row_hi, team, teams;
@@ -185,33 +188,15 @@ struct Work {
         h = __builtin_amdgcn_readfirstlane(h);
         off = uniform(rem - before(now, tile));
         u0 = lo - off;
-    }
-    // The next piece of my share; false: there is none.
-    __device__ __forceinline__ bool next(Unit& u, int lane)
-    {
-        if (!(left > 0.0)) return false;
-        const double cost = base + (tile + 1) * inc, take_ = fmin(cost - off, left), end = off + take_;
-        if (end < cost && end <= OVERHEAD) return false;       // my share ends ahead of its first key
-        u.first = first; u.G = G; u.rows = n * G; u.pos0 = pos0; u.seq = seq; u.h = h; u.row0 = tile * R;
-        u.tok0 = __builtin_amdgcn_readfirstlane(u.row0 / G);
-        u.rem0 = __builtin_amdgcn_readfirstlane(u.row0 - u.tok0 * G);
-        u.inv_g = inv_g;
-        u.ke = min(max(u.pos(min(R, u.rows - u.row0) - 1) + 1, 0), most_keys);
-        u.kb = window > 0 ? min(max(u.pos(0) + 1 - window, 0), u.ke) : 0;
-        const int runs = (u.ke - (u.kb & ~(RUN - 1)) + RUN - 1) / RUN;
-        u.r0 = 0; u.r1 = runs; u.pieces = 1; u.piece = 0; u.team0 = team;
-        if (off > OVERHEAD || end < cost) {
-            const double per_cost = runs / (cost - OVERHEAD);
-            if (off > OVERHEAD) u.r0 = min((int)((off - OVERHEAD) * per_cost), runs);
-            if (end < cost) u.r1 = min((int)((end - OVERHEAD) * per_cost), runs);
-            u.team0 = min(max((int)((u0 + OVERHEAD) / chunk), 0), team);
-            u.pieces = min((int)((u0 + cost - 1.0) / chunk), teams - 1) - u.team0 + 1;
-            u.piece = team - u.team0;
+        const double cost = base + (tile + 1) * inc;
+        if (off > HEAD && cost - off <= TAIL) {                // the team before takes the rest of it along
+            left -= cost - off;
+            advance(cost, lane);
         }
-        auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
-        scalar(u.first); scalar(u.rows); scalar(u.pos0); scalar(u.seq); scalar(u.h); scalar(u.row0); scalar(u.kb); scalar(u.ke);
-        scalar(u.r0); scalar(u.r1); scalar(u.pieces); scalar(u.piece); scalar(u.team0);
-        left -= take_;
+    }
+    // on to the next unit
+    __device__ __forceinline__ void advance(double cost, int lane)
+    {
         off = 0.0;
         u0 += cost;
         if (left > 0.0 && ++tile == ntile) {
@@ -225,6 +210,38 @@ struct Work {
                 } while (n == 0);
             }
         }
+    }
+    // The next piece of my share; false: there is none.
+    __device__ __forceinline__ bool next(Unit& u, int lane)
+    {
+        if (!(left > 0.0)) return false;
+        const double cost = base + (tile + 1) * inc, take_ = fmin(cost - off, left), end = off + take_;
+        if (end < cost && end <= HEAD) return false;           // the next team's
+        u.first = first; u.G = G; u.rows = n * G; u.pos0 = pos0; u.seq = seq; u.h = h; u.row0 = tile * R;
+        u.tok0 = __builtin_amdgcn_readfirstlane(u.row0 / G);
+        u.rem0 = __builtin_amdgcn_readfirstlane(u.row0 - u.tok0 * G);
+        u.inv_g = inv_g;
+        u.ke = min(max(u.pos(min(R, u.rows - u.row0) - 1) + 1, 0), most_keys);
+        u.kb = window > 0 ? min(max(u.pos(0) + 1 - window, 0), u.ke) : 0;
+        const int runs = (u.ke - (u.kb & ~(RUN - 1)) + RUN - 1) / RUN;
+        u.r0 = 0; u.r1 = runs; u.pieces = 1; u.piece = 0; u.team0 = team;
+        if (off > HEAD || end < cost - TAIL) {
+            u.team0 = min(max((int)((u0 + HEAD) / chunk), 0), team);
+            const int last = max(min((int)((u0 + cost - 1.0 - TAIL) / chunk), teams - 1), team);
+            u.pieces = last - u.team0 + 1;
+            u.piece = team - u.team0;
+            const double lo0 = u.team0 * chunk;
+            const double w0 = u0 <= lo0 ? chunk : lo0 + chunk - u0 - (u0 - lo0 > TAIL ? OVERHEAD : 0);   // > 0: HEAD exceeds OVERHEAD
+            const double all = w0 + (last - u.team0) * chunk - (last > u.team0 ? (last + 1) * chunk - (u0 + cost) : 0.0);
+            const double c0 = u.piece == 0 ? 0.0 : w0 + (u.piece - 1) * chunk, c1 = u.piece == 0 ? w0 : c0 + chunk, per = runs / all;
+            u.r0 = min((int)(c0 * per), runs);
+            if (team < last) u.r1 = min((int)(c1 * per), runs);
+        }
+        auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
+        scalar(u.first); scalar(u.rows); scalar(u.pos0); scalar(u.seq); scalar(u.h); scalar(u.row0); scalar(u.kb); scalar(u.ke);
+        scalar(u.r0); scalar(u.r1); scalar(u.pieces); scalar(u.piece); scalar(u.team0);
+        left -= take_;
+        advance(cost, lane);
         return true;
     }
     // which of a team's two slots a piece of a shared unit uses: the unit it ends with, or the one it begins with

@@ -445,7 +445,10 @@ typedef struct infmllm_batch {
 
 enum {
     INFMLLM_PAGED_SCALE = 0,  /* softmax scale on q.k; default 1/sqrt(head_dim)                                   */
-    INFMLLM_PAGED_WINDOW = 1  /* a token sees the newest `window` keys, itself included; 0 (default): all          */
+    INFMLLM_PAGED_WINDOW = 1, /* a token sees the newest `window` keys, itself included; 0 (default): all          */
+    INFMLLM_PAGED_KERNEL = 2  /* debug/test, bf16: 0 (default) = the attention picks its kernel; 1 = the one for few rows, 2 = that for
+                                 chunks, 3 = both side by side (the first for sequences of at most 16 rows).  Results are the
+                                 same up to the rounding of weights                                              */
 };
 
 /*

@@ -32,7 +32,7 @@ EXPORTS = [
 ]
 ROTARY_BASE, ROTARY_DIMS, ROTARY_LAYOUT, ROTARY_FACTOR, ROTARY_TRAINED, ROTARY_LOW, ROTARY_HIGH, ROTARY_MAGNITUDE, ROTARY_EPS = range(9)
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
-PAGED_SCALE, PAGED_WINDOW = 0, 1
+PAGED_SCALE, PAGED_WINDOW, PAGED_KERNEL = 0, 1, 2
 STATIC_WORKSPACE_BYTES = 64 << 20
 KERNELS = ["append", "attn", "score", "select", "compact", "decode", "rope", "evict"]
 
@@ -456,7 +456,7 @@ class PagedCache(_Attached):
     """infmllm_paged_t with its workspace: geometry and scratch of a paged cache; the pools of a layer, [pages, kv_heads,
     page_size, head_dim] each, are the caller's and are arguments of every call (pools() makes a pair)."""
 
-    def __init__(self, pages, page_size, heads, kv_heads, head_dim, dtype=torch.bfloat16, scale=None, window=None, device="cuda:0",
+    def __init__(self, pages, page_size, heads, kv_heads, head_dim, dtype=torch.bfloat16, scale=None, window=None, kernel=None, device="cuda:0",
                  hip_stream=None):
         L = lib()
         self.heads, self.kv_heads, self.head_dim, self.dtype = heads, kv_heads, head_dim, dtype
@@ -464,7 +464,7 @@ class PagedCache(_Attached):
         h = ctypes.c_void_p()
         _check(L.infmllm_paged_create(pages, page_size, heads, kv_heads, head_dim, _dtype_code(dtype), ctypes.byref(h)))
         self._h, self._destroy = h, L.infmllm_paged_destroy
-        for which, val in ((PAGED_SCALE, scale), (PAGED_WINDOW, window)):
+        for which, val in ((PAGED_SCALE, scale), (PAGED_WINDOW, window), (PAGED_KERNEL, kernel)):
             if val is not None:
                 _check(L.infmllm_paged_set_param(h, which, float(val)))
         self._attach("infmllm_paged", h, device, hip_stream)

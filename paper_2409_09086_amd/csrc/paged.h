@@ -45,9 +45,9 @@ struct PagedScratch { float* part; int* arrived; };
 constexpr int PAGED_CUS = 256;                     // compute units: teams of a launch with one a CU
 constexpr int PAGED_TEAMS = 8 * PAGED_CUS;         // most teams of a launch
 
-// Few rows a unit: 16 or 32; max_new: the caller's bound.
+// Few rows a unit: 16 or 32; max_new, max_len: the caller's bounds.
 template <typename T>
-hipError_t launch_paged_rows(const PagedArgs<T>& a, const PagedScratch& sc, int head_dim, int max_new, hipStream_t st);
+hipError_t launch_paged_rows(const PagedArgs<T>& a, const PagedScratch& sc, int head_dim, int max_new, int max_len, hipStream_t st);
 size_t paged_rows_scratch(int head_dim, int elt);  // bytes of PagedScratch::part
 // The same for bf16 chunks of many rows, 256 a unit.
 hipError_t launch_paged_fwd(const PagedArgs<uint16_t>& a, const PagedScratch& sc, int head_dim, hipStream_t st);

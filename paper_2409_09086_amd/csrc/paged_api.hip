@@ -68,6 +68,27 @@ int check_batch(const char* who, const infmllm_batch_t* b)
 
 bool whole(double v) { return v == std::floor(v); }
 
+// Whether the kernel for few rows (32 a unit) is the faster one for bf16 queries, by what the two should take, in us.  It reads the keys once
+// for every 32 rows; where there are no more units than teams those of one head run beside each other and find them in the L2, otherwise they
+// come from behind it, at 6 TB/s.  The kernel for chunks takes some 40 us for a grid that its units do not fill (pieces and
+// their merge), else 14 and its tiles of 256 rows by 64 keys.  Measured, us, few rows / chunks, heads of 128 in groups of 4, rows of a
+// sequence: 1 x 8000 keys, 8 kv-heads, 64 rows 24.1 / 44.6, 256 27.4 / 46.5; 4 x 4000, 8, 256 37.6 / 44.4; 16 x 4000, 8, 32 55.8 / 66.3,
+// 64 56.7 / 67.4, 96 123.0 / 69.3; 16 x 4000, 2, 256 38.0 / 43.8; 32 x 2000, 8, 32 52.6 / 56.4, 64 90.4 / 57.5; 32 x 2000, 2, 128 25.0 / 38.4,
+// 256 44.2 / 41.3; of 64: 16 x 4000, 8, 64 27.9 / 47.0, 96 61.8 / 49.1; 4 x 4000, 8, 256 27.1 / 32.4.
+template <typename T>
+bool few_rows_pay(const PagedArgs<T>& a, int d, int max_new, int max_len)
+{
+    const double rows = (double)std::min(max_new, a.tokens) * a.G, keys = std::min((double)max_len, (double)a.pages_per_seq * (1 << a.page_shift));
+    if (rows <= 32) return true;
+    const double seqs = std::min(a.seqs, a.tokens), all = (double)a.tokens * a.G;
+    auto units = [&](int block) { return a.Hkv * std::min(seqs * std::ceil(rows / block), all / block + seqs); };
+    const double memory = seqs * a.Hkv * keys * 4 * d / 5.3e6, few = units(32) * keys;
+    const double t_few = units(32) <= PAGED_CUS ? (d == 128 ? 12 : 10) + std::max(memory, few / (d == 128 ? 43e3 : 60e3)) : 14 + few * 4 * d / 6e6;
+    const double tiles = units(256) * keys / 64 / PAGED_CUS;
+    const double t_many = std::max(d == 128 ? 40.0 : 28.0, (d == 128 ? 14 : 10) + std::max(memory, tiles * (d == 128 ? 1.75 : 1.0)));
+    return t_few < t_many;
+}
+
 }  // namespace
 
 struct infmllm_rotary {
@@ -91,7 +112,7 @@ struct infmllm_rotary {
 };
 
 struct infmllm_paged {
-    int pages, page_size, page_shift, Hq, Hkv, d, dtype, window = 0;
+    int pages, page_size, page_shift, Hq, Hkv, d, dtype, window = 0, kernel = 0;
     double scale;
     bool attached = false;
     int dev = 0;
@@ -272,6 +293,10 @@ int infmllm_paged_set_param(infmllm_paged_t* p, int which, double value)
                 return fail(INFMLLM_EINVAL, "paged_set_param: window must be an integer in 0..2^30");
             p->window = (int)value;
             return INFMLLM_OK;
+        case INFMLLM_PAGED_KERNEL:
+            if (value != 0 && value != 1 && value != 2 && value != 3) return fail(INFMLLM_EINVAL, "paged_set_param: kernel must be 0, 1, 2 or 3");
+            p->kernel = (int)value;
+            return INFMLLM_OK;
         default:
             return fail(INFMLLM_EINVAL, "paged_set_param: unknown parameter %d", which);
     }
@@ -370,14 +395,16 @@ int infmllm_paged_attend(infmllm_paged_t* p, const infmllm_batch_t* batch, const
         a.inv_g = (uint32_t)((1ull << 32) / (unsigned)a.G + 1);
         a.c = (float)(p->scale * 1.4426950408889634);
         if constexpr (sizeof(T) == 2) {
-            // Chunks of more than a few rows run 256 rows a unit; beside them sequences whose rows are one block of 16 run on their own.
-            const int new_max = std::min(batch->max_new, batch->tokens), few = 16;
-            if ((int64_t)new_max * a.G > 2 * few) {
-                const bool alike = a.seqs == 1 || (int64_t)new_max * a.seqs == a.tokens;
-                return alike ? launch_paged_fwd(a, p->sc, p->d, p->st) : launch_paged_mixed(a, p->sc, p->d, few, p->st);
+            const int few = 16;                                // rows of sequences that run on their own beside chunks
+            int kernel = p->kernel;
+            if (kernel == 0) {
+                const bool alike = a.seqs == 1 || (int64_t)std::min(batch->max_new, a.tokens) * a.seqs == a.tokens;
+                kernel = few_rows_pay(a, p->d, batch->max_new, batch->max_len) ? 1 : alike ? 2 : 3;
             }
+            if (kernel == 2) return launch_paged_fwd(a, p->sc, p->d, p->st);
+            if (kernel == 3) return launch_paged_mixed(a, p->sc, p->d, few, p->st);
         }
-        return launch_paged_rows<T>(a, p->sc, p->d, batch->max_new, p->st);
+        return launch_paged_rows<T>(a, p->sc, p->d, batch->max_new, batch->max_len, p->st);
     };
     const hipError_t e = elt == 2 ? go((uint16_t*)nullptr) : go((float*)nullptr);
     return e == hipSuccess ? INFMLLM_OK : fail_hip(e, who);

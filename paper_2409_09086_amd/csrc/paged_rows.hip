@@ -15,6 +15,7 @@
 // wavefront: see the launch for which.
 #include <algorithm>
 #include <climits>
+#include <cmath>
 
 #include "paged_rows.h"
 
@@ -34,7 +35,8 @@ paged_rows_kernel(PagedArgs<T> a, PagedScratch sc, int least)
     {
         W work;
         const auto sums = work.measure(a, &sh.win[wave], 0, INT_MAX, lane);
-        work.begin(sums, blockIdx.x, gridDim.x, least, lane);
+        // Neighbouring shares may read the same keys: XCD x (workgroups of one residue class mod 8) gets the x-th eighth of them.
+        work.begin(sums, (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3), gridDim.x, least, lane);
         sh.place[wave] = work;
     }
     rows_body<T, D, NRB, TW, 1>(a, sc.part, sc.arrived, smem, sh);
@@ -48,28 +50,31 @@ hipError_t launch(const PagedArgs<T>& a, const PagedScratch& sc, int teams, int 
 }
 
 template <typename T, int D>
-hipError_t launch_d(const PagedArgs<T>& a, const PagedScratch& sc, int max_new, hipStream_t st)
+hipError_t launch_d(const PagedArgs<T>& a, const PagedScratch& sc, int max_new, int max_len, hipStream_t st)
 {
     constexpr int KEYS = RowsKernel<T, D, 1>::KEYS;
     const int64_t rows = (int64_t)std::max(1, std::min(max_new, a.tokens)) * a.G;
     const int64_t units = (int64_t)std::min(a.seqs, a.tokens) * a.Hkv * ((rows + 15) / 16);
+    // The smallest share.  Halving it halves the time that a team takes for its keys (4 D bytes each at some 40 GB/s) and doubles that of
+    // the one which merges a unit's pieces (4 D bytes a row and piece at some 80 GB/s): sqrt(keys * rows / 2).
+    auto least = [&](int block) { return std::max(4 * KEYS, (int)std::sqrt(0.5 * max_len * (double)std::min<int64_t>(rows, block))); };
     if constexpr (sizeof(T) == 2) {
-        if (rows > 16) return launch<T, D, 2, 8>(a, sc, PAGED_CUS, 4 * KEYS, st);
+        if (rows > 16) return launch<T, D, 2, 8>(a, sc, PAGED_CUS, least(32), st);
     }
     if (units >= 4 * PAGED_CUS) return launch<T, D, 1, 1>(a, sc, 8 * PAGED_CUS, 2 * KEYS, st);
-    return launch<T, D, 1, 8>(a, sc, PAGED_CUS, 4 * KEYS, st);
+    return launch<T, D, 1, 8>(a, sc, PAGED_CUS, least(16), st);
 }
 
 }  // namespace
 
 template <typename T>
-hipError_t launch_paged_rows(const PagedArgs<T>& a, const PagedScratch& sc, int head_dim, int max_new, hipStream_t st)
+hipError_t launch_paged_rows(const PagedArgs<T>& a, const PagedScratch& sc, int head_dim, int max_new, int max_len, hipStream_t st)
 {
-    if (head_dim == 128) return launch_d<T, 128>(a, sc, max_new, st);
-    return launch_d<T, 64>(a, sc, max_new, st);
+    if (head_dim == 128) return launch_d<T, 128>(a, sc, max_new, max_len, st);
+    return launch_d<T, 64>(a, sc, max_new, max_len, st);
 }
-template hipError_t launch_paged_rows<uint16_t>(const PagedArgs<uint16_t>&, const PagedScratch&, int, int, hipStream_t);
-template hipError_t launch_paged_rows<float>(const PagedArgs<float>&, const PagedScratch&, int, int, hipStream_t);
+template hipError_t launch_paged_rows<uint16_t>(const PagedArgs<uint16_t>&, const PagedScratch&, int, int, int, hipStream_t);
+template hipError_t launch_paged_rows<float>(const PagedArgs<float>&, const PagedScratch&, int, int, int, hipStream_t);
 
 size_t paged_rows_scratch(int head_dim, int elt)
 {

@@ -58,7 +58,8 @@ def test_parameters_and_states():
     assert L.infmllm_rotary_attach(r, ONE, 1 << 30, None) == B.EINVAL
     rc, p = paged()
     assert rc == B.OK
-    for which, bad, ok in [(B.PAGED_SCALE, (0.0, -1.0), (0.1,)), (B.PAGED_WINDOW, (-1.0, 1.5, 2.0 ** 31), (0.0, 1.0, 4096.0))]:
+    for which, bad, ok in [(B.PAGED_SCALE, (0.0, -1.0), (0.1,)), (B.PAGED_WINDOW, (-1.0, 1.5, 2.0 ** 31), (0.0, 1.0, 4096.0)),
+                           (B.PAGED_KERNEL, (-1.0, 4.0, 0.5), (1.0, 2.0, 3.0, 0.0))]:
         for v in bad + (float("nan"), float("inf")):
             assert L.infmllm_paged_set_param(p, which, v) == B.EINVAL, (which, v)
         for v in ok:

@@ -395,7 +395,7 @@ int infmllm_rotary_attach(infmllm_rotary_t* r, void* dev_workspace, size_t bytes
  *   positions   device, int32 [tokens]; the rows of a token outside 0 .. max_positions - 1 become NaN where they are turned
  *   q, q_out    device, token i's `heads` heads of head_dim at i * q_stride (q_out_stride) elements, dense within the token.
  *               May be null together with heads = 0
- *   k, k_out    the same with kv_heads
+ *   k, k_out    the same with kv_heads; at most 16384 of either
  *   q_weight    device, [head_dim] in the object's dtype: the norm's weights; null: no norm of the queries
  *   k_weight    the same for the keys
  * Data pointers are aligned to 16 bytes and strides are multiples of 16 bytes, at least a token's heads.  An output may be its
@@ -453,7 +453,7 @@ enum {
 
 /*
  * Creates a paged object: pools of `pages` pages (1..2^30) of page_size rows (a power of two in 16..1024); heads, kv_heads,
- * head_dim and dtype as for infmllm_stream_create, at most 65536 heads and 4096 of a group, and pages of all kv-heads below 2^29
+ * head_dim and dtype as for infmllm_stream_create, at most 16384 heads and 4096 of a group, and pages of all kv-heads below 2^29
  * elements.  Host-only.  Errors: EINVAL, ENOMEM.
  */
 int infmllm_paged_create(int pages, int page_size, int heads, int kv_heads, int head_dim, int dtype, infmllm_paged_t** out);

@@ -334,10 +334,10 @@ def _dtype_code(dtype):
     return code
 
 
-def _rows(t, dtype, tokens, heads, head_dim, name):
+def _rows(t, dtype, dev, tokens, heads, head_dim, name):
     """Address and token stride of a [tokens, heads, head_dim] tensor whose tokens are dense."""
-    if t.dtype != dtype or not t.is_cuda:
-        raise ValueError("%s must be a device tensor of dtype %s" % (name, dtype))
+    if t.dtype != dtype or t.device != dev:
+        raise ValueError("%s must be a tensor of dtype %s on %s" % (name, dtype, dev))
     if t.shape != (tokens, heads, head_dim):
         raise ValueError("%s must have shape %s (got %s)" % (name, (tokens, heads, head_dim), tuple(t.shape)))
     s0, s1, s2 = t.stride()
@@ -346,17 +346,11 @@ def _rows(t, dtype, tokens, heads, head_dim, name):
     return t.data_ptr(), s0 if tokens > 1 else max(s0, heads * head_dim)
 
 
-def _pool(t, dtype, shape, name):
-    """Address of a dense tensor (as _dev_ptr, without its objects: the calls below are short)."""
-    if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous device tensor of shape %s and dtype %s" % (name, tuple(shape), dtype))
+def _dense(t, dtype, dev, shape, name):
+    """Address of a dense tensor."""
+    if t.dtype != dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor of shape %s and dtype %s on %s" % (name, tuple(shape), dtype, dev))
     return t.data_ptr()
-
-
-def _weight(w, dtype, head_dim, name):
-    if not w.is_cuda or w.dtype != dtype or w.shape != (head_dim,) or not w.is_contiguous():
-        raise ValueError("%s must be a contiguous device tensor of %d elements of dtype %s" % (name, head_dim, dtype))
-    return w.data_ptr()
 
 
 class _Attached:
@@ -370,6 +364,7 @@ class _Attached:
         with torch.cuda.device(self.device):
             self.hip_stream = hip_stream if hip_stream is not None else torch.cuda.current_stream(self.device).cuda_stream
             self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+            self.device = self.workspace.device                # with its index
             aligned = (self.workspace.data_ptr() + 255) // 256 * 256
             _check(getattr(L, prefix + "_attach")(handle, ctypes.c_void_p(aligned), nbytes, ctypes.c_void_p(self.hip_stream)))
 
@@ -407,26 +402,25 @@ class Rotary(_Attached):
     def apply(self, positions, q=None, k=None, q_weight=None, k_weight=None, q_out=None, k_out=None):
         """infmllm_rotary_apply: q [n, heads, d], k [n, kv_heads, d] (either may be None), positions int32 [n].
         Returns (q_out, k_out); q_out=q turns in place.  Nothing is synchronised."""
-        n, d, dt = positions.shape[0], self.head_dim, self.dtype
-        if positions.dtype != torch.int32 or positions.dim() != 1 or not positions.is_cuda or not positions.is_contiguous():
-            raise ValueError("positions must be a contiguous device tensor of int32 [n]")
+        n, d, dt, dev = positions.shape[0], self.head_dim, self.dtype, self.device
+        pos = _dense(positions, torch.int32, dev, (n,), "positions")
         heads = kv_heads = qs = ks = qos = kos = 0
         qp = kp = qo = ko = None
         if q is not None:
             heads = q.shape[1]
             if q_out is None:
                 q_out = torch.empty_like(q)
-            qp, qs = _rows(q, dt, n, heads, d, "q")
-            qo, qos = _rows(q_out, dt, n, heads, d, "q_out")
+            qp, qs = _rows(q, dt, dev, n, heads, d, "q")
+            qo, qos = _rows(q_out, dt, dev, n, heads, d, "q_out")
         if k is not None:
             kv_heads = k.shape[1]
             if k_out is None:
                 k_out = torch.empty_like(k)
-            kp, ks = _rows(k, dt, n, kv_heads, d, "k")
-            ko, kos = _rows(k_out, dt, n, kv_heads, d, "k_out")
-        _check(_lib.infmllm_rotary_apply(self._h, positions.data_ptr(), n, heads, kv_heads, qp, qs, kp, ks,
-                                         None if q_weight is None else _weight(q_weight, dt, d, "q_weight"),
-                                         None if k_weight is None else _weight(k_weight, dt, d, "k_weight"), qo, qos, ko, kos))
+            kp, ks = _rows(k, dt, dev, n, kv_heads, d, "k")
+            ko, kos = _rows(k_out, dt, dev, n, kv_heads, d, "k_out")
+        _check(_lib.infmllm_rotary_apply(self._h, pos, n, heads, kv_heads, qp, qs, kp, ks,
+                                         None if q_weight is None else _dense(q_weight, dt, dev, (d,), "q_weight"),
+                                         None if k_weight is None else _dense(k_weight, dt, dev, (d,), "k_weight"), qo, qos, ko, kos))
         return (None if q is None else q_out), (None if k is None else k_out)
 
 
@@ -443,9 +437,11 @@ class PagedBatch:
         seqs = lens.shape[0]
         if table.dim() != 2:
             raise ValueError("table must be two-dimensional")
-        _dev_ptr(starts, torch.int32, (seqs + 1,), "starts")
-        _dev_ptr(lens, torch.int32, (seqs,), "lens")
-        _dev_ptr(table, torch.int32, (seqs, table.shape[1]), "table")
+        self.device = lens.device
+        if not lens.is_cuda:
+            raise ValueError("a batch's arrays must be device tensors")
+        for t, shape, name in ((starts, (seqs + 1,), "starts"), (lens, (seqs,), "lens"), (table, (seqs, table.shape[1]), "table")):
+            _dense(t, torch.int32, self.device, shape, name)
         self.starts, self.lens, self.table = starts, lens, table
         self.tokens = int(tokens)
         self._c = _Batch(seqs, self.tokens, int(max_new), int(max_len), starts.data_ptr(), lens.data_ptr(), table.data_ptr(), table.shape[1])
@@ -476,30 +472,34 @@ class PagedCache(_Attached):
     def append(self, batch, k, v, K, V, rotary=None, k_weight=None, q=None, q_weight=None, q_out=None):
         """infmllm_paged_append: k, v [tokens, kv_heads, d] enter the pools K, V; with a Rotary, keys and (where given) queries q
         [tokens, heads, d] are normed and turned on the way.  Returns q_out (None without q).  Nothing is synchronised."""
-        n, d, dt = batch.tokens, self.head_dim, self.dtype
+        n, d, dt, dev = batch.tokens, self.head_dim, self.dtype, self.device
+        if batch.device != dev or (rotary is not None and rotary._h is None):
+            raise ValueError("the batch must be on %s, the rotary object open" % dev)
         qs = qos = 0
         qp = qo = None
         if q is not None:
             if q_out is None:
                 q_out = torch.empty_like(q)
-            qp, qs = _rows(q, dt, n, self.heads, d, "q")
-            qo, qos = _rows(q_out, dt, n, self.heads, d, "q_out")
-        kp, ks = _rows(k, dt, n, self.kv_heads, d, "k")
-        vp, vs = _rows(v, dt, n, self.kv_heads, d, "v")
+            qp, qs = _rows(q, dt, dev, n, self.heads, d, "q")
+            qo, qos = _rows(q_out, dt, dev, n, self.heads, d, "q_out")
+        kp, ks = _rows(k, dt, dev, n, self.kv_heads, d, "k")
+        vp, vs = _rows(v, dt, dev, n, self.kv_heads, d, "v")
         _check(_lib.infmllm_paged_append(self._h, None if rotary is None else rotary._h, batch._ref, kp, ks, vp, vs,
-                                         None if k_weight is None else _weight(k_weight, dt, d, "k_weight"), qp, qs,
-                                         None if q_weight is None else _weight(q_weight, dt, d, "q_weight"), qo, qos,
-                                         _pool(K, dt, self.pool_shape, "K"), _pool(V, dt, self.pool_shape, "V")))
+                                         None if k_weight is None else _dense(k_weight, dt, dev, (d,), "k_weight"), qp, qs,
+                                         None if q_weight is None else _dense(q_weight, dt, dev, (d,), "q_weight"), qo, qos,
+                                         _dense(K, dt, dev, self.pool_shape, "K"), _dense(V, dt, dev, self.pool_shape, "V")))
         return q_out if q is not None else None
 
     def attend(self, batch, q, K, V, out=None, lse=None):
         """infmllm_paged_attend: attention of q [tokens, heads, d] over the batch's pages.  Returns out [tokens, heads, d]; lse, float
         [tokens, heads], receives the log-sum-exp.  Nothing is synchronised."""
-        n, d, dt = batch.tokens, self.head_dim, self.dtype
-        qp, qs = _rows(q, dt, n, self.heads, d, "q")
+        n, d, dt, dev = batch.tokens, self.head_dim, self.dtype, self.device
+        if batch.device != dev:
+            raise ValueError("the batch must be on %s" % dev)
+        qp, qs = _rows(q, dt, dev, n, self.heads, d, "q")
         if out is None:
             out = torch.empty((n, self.heads, d), dtype=dt, device=q.device)
-        _check(_lib.infmllm_paged_attend(self._h, batch._ref, qp, qs, _pool(K, dt, self.pool_shape, "K"), _pool(V, dt, self.pool_shape, "V"),
-                                         _pool(out, dt, (n, self.heads, d), "out"),
-                                         None if lse is None else _pool(lse, torch.float32, (n, self.heads), "lse")))
+        _check(_lib.infmllm_paged_attend(self._h, batch._ref, qp, qs, _dense(K, dt, dev, self.pool_shape, "K"), _dense(V, dt, dev, self.pool_shape, "V"),
+                                         _dense(out, dt, dev, (n, self.heads, d), "out"),
+                                         None if lse is None else _dense(lse, torch.float32, dev, (n, self.heads), "lse")))
         return out

@@ -222,8 +222,8 @@ int infmllm_rotary_apply(infmllm_rotary_t* r, const int32_t* positions, int toke
     if (!r->attached) return fail(INFMLLM_ESTATE, "%s: the object has no workspace attached", who);
     if (tokens < 0 || tokens > (1 << 24)) return fail(INFMLLM_EINVAL, "%s: tokens must lie in 0..2^24 (got %d)", who, tokens);
     if (tokens == 0) return INFMLLM_OK;
-    if (heads < 0 || kv_heads < 0 || heads > 65536 || kv_heads > 65536 || heads + kv_heads == 0)
-        return fail(INFMLLM_EINVAL, "%s: heads and kv_heads must lie in 0..65536, not both 0 (got %d, %d)", who, heads, kv_heads);
+    if (heads < 0 || kv_heads < 0 || heads > 16384 || kv_heads > 16384 || heads + kv_heads == 0)
+        return fail(INFMLLM_EINVAL, "%s: heads and kv_heads must lie in 0..16384, not both 0 (got %d, %d)", who, heads, kv_heads);
     if (!positions || (uintptr_t)positions % 4) return fail(INFMLLM_EINVAL, "%s: positions must not be null and be aligned to 4 bytes", who);
     const int elt = r->dtype == INFMLLM_BF16 ? 2 : 4;
     int rc;
@@ -261,8 +261,8 @@ int infmllm_paged_create(int pages, int page_size, int heads, int kv_heads, int 
     if (pages < 1 || pages > (1 << 30)) return fail(INFMLLM_EINVAL, "paged_create: pages must lie in 1..2^30 (got %d)", pages);
     if (page_size < 16 || page_size > 1024 || (page_size & (page_size - 1)))
         return fail(INFMLLM_EINVAL, "paged_create: page_size must be a power of two in 16..1024 (got %d)", page_size);
-    if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || heads > 65536)
-        return fail(INFMLLM_EINVAL, "paged_create: kv_heads must divide heads, at most 65536 (got %d, %d)", heads, kv_heads);
+    if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || heads > 16384)
+        return fail(INFMLLM_EINVAL, "paged_create: kv_heads must divide heads, at most 16384 (got %d, %d)", heads, kv_heads);
     if (heads / kv_heads > 4096) return fail(INFMLLM_EINVAL, "paged_create: at most 4096 heads share a kv-head (got %d)", heads / kv_heads);
     if (head_dim != 64 && head_dim != 128)
         return fail(INFMLLM_EINVAL, "paged_create: head_dim must be 64 or 128 (got %d)", head_dim);
@@ -340,6 +340,7 @@ int infmllm_paged_append(infmllm_paged_t* p, infmllm_rotary_t* rotary, const inf
     } else if (q || k_weight || q_weight) {
         return fail(INFMLLM_EINVAL, "%s: queries and norm weights need a rotary object", who);
     }
+    if (q_weight && !q) return fail(INFMLLM_EINVAL, "%s: q_weight without q", who);
     const int elt = p->elt();
     if ((rc = check_rows(who, "k", k, k_stride, p->Hkv, p->d, elt)) || (rc = check_rows(who, "v", v, v_stride, p->Hkv, p->d, elt)) ||
         (rc = check_weight(who, "k_weight", k_weight)) || (rc = check_weight(who, "q_weight", q_weight)))

@@ -26,7 +26,7 @@ def test_rotary_create_refuses(args):
 
 @pytest.mark.parametrize("args", [dict(pages=0), dict(pages=(1 << 30) + 1), dict(page=8), dict(page=24), dict(page=2048), dict(heads=3), dict(heads=0),
                                   dict(kv=0), dict(kv=-2), dict(d=96), dict(dtype=2), dict(heads=1 << 17),
-                                  dict(heads=8192, kv=1), dict(heads=65536, kv=65536, page=1024, d=128)])
+                                  dict(heads=8192, kv=1), dict(heads=16384, kv=16384, page=1024, d=128)])
 def test_paged_create_refuses(args):
     rc, h = paged(**args)
     assert rc == B.EINVAL and not h.value and B.last_error()
@@ -89,7 +89,7 @@ def test_calls_of_attached_objects_refuse():
     apply = lambda **k: L.infmllm_rotary_apply(*[k.get(n, v) for n, v in dict(
         r=rot._h, pos=ONE, tokens=4, heads=4, kv=2, q=ONE, qs=256, k=ONE, ks=128, qw=None, kw=None, qo=ONE, qos=256, ko=ONE, kos=128).items()])
     odd = ctypes.c_void_p(264)
-    for bad in [dict(r=None), dict(pos=None), dict(pos=ctypes.c_void_p(258)), dict(tokens=-1), dict(heads=-1), dict(heads=0, kv=0), dict(q=None), dict(k=None),
+    for bad in [dict(r=None), dict(pos=None), dict(pos=ctypes.c_void_p(258)), dict(tokens=-1), dict(heads=-1), dict(heads=0, kv=0), dict(heads=16385), dict(kv=1 << 20), dict(q=None), dict(k=None),
                 dict(qo=None), dict(ko=None), dict(q=odd), dict(k=odd), dict(qo=odd), dict(qs=255), dict(qs=248), dict(ks=132), dict(kos=0),
                 dict(qw=odd), dict(kw=odd)]:
         assert apply(**bad) == B.EINVAL, bad
@@ -114,7 +114,7 @@ def test_calls_of_attached_objects_refuse():
     for bad in [dict(p=None), dict(k=None), dict(v=None), dict(k=odd), dict(v=odd), dict(ks=64), dict(vs=130), dict(q=odd), dict(qo=None), dict(qos=128),
                 dict(K=None), dict(V=None), dict(K=odd), dict(kw=odd), dict(qw=odd), dict(r=None), dict(r=other._h)]:
         assert append(**bad) == B.EINVAL, bad
-    assert append(r=None, q=None, kw=ONE) == B.EINVAL
+    assert append(r=None, q=None, kw=ONE) == B.EINVAL and append(q=None, qw=ONE) == B.EINVAL
     assert append(r=short._h) == B.ECAPACITY
     for bad in [dict(p=None), dict(q=None), dict(q=odd), dict(qs=128), dict(qs=260), dict(K=None), dict(V=odd), dict(out=None), dict(out=odd),
                 dict(lse=ctypes.c_void_p(258))]:
@@ -144,4 +144,13 @@ def test_binding_refuses_what_it_cannot_pass_on():
     with pytest.raises(ValueError):
         B.PagedBatch(i32(0, 2), i32(5, 6), i32(1).reshape(1, 1), 2, 2, 5)
     with pytest.raises(ValueError):
+        B.PagedBatch(torch.tensor([0, 2], dtype=torch.int32), torch.tensor([5], dtype=torch.int32), torch.ones((1, 1), dtype=torch.int32), 2, 2, 5)
+    with pytest.raises(ValueError):
         B.Rotary(64, 100, layout="other")
+    k = q[:, :2].contiguous()
+    rot.close()
+    with pytest.raises(ValueError):                            # not a cache without rotation by accident
+        cache.append(b, k, k, K, V, rotary=rot)
+    with pytest.raises(B.InfMLLMError):
+        rot.apply(i32(1, 2), q)
+    assert B.PagedCache(8, 16, 4, 2, 64, device="cuda").device == torch.device("cuda:0")

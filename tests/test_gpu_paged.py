@@ -146,6 +146,7 @@ class Case:
 
 
 KERNELS = [0, 1, 2, 3]     # its own choice; that for few rows, that for chunks, both
+TYPES = [("bf16", k) for k in KERNELS] + [("fp32", 0)]
 
 ATTEND = [
     # dtype, heads, kv, d, page, window, [(new, len)]
@@ -170,11 +171,8 @@ ATTEND = [
 ]
 
 
-@pytest.mark.parametrize("dtype,heads,kv,d,page,window,seqs", ATTEND)
-@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("dtype,heads,kv,d,page,window,seqs,kernel", [c + (k,) for c in ATTEND for k in (KERNELS if c[0] == "bf16" else [0])])
 def test_attend(dtype, heads, kv, d, page, window, seqs, kernel):
-    if dtype == "fp32" and kernel:
-        pytest.skip("one kernel")
     print("attend", dtype, heads, kv, d, page, window, seqs, kernel, flush=True)
     c = Case(len(seqs) + heads, dtype, heads, kv, d, page, seqs, window, tail=3)
     cache = c.cache(kernel=kernel)
@@ -203,14 +201,11 @@ def test_many_sequences(seqs, share, chunk, window, kernel):
     c.check(out, lse)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dtype,kernel", TYPES)
 @pytest.mark.parametrize("what", ["value", "key"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("kernel", KERNELS)
 def test_hidden_rows_reach_no_result(dtype, what, bad, kernel):
     """A new token whose key or value is not finite: only the rows that see it may show it."""
-    if dtype == "fp32" and kernel:
-        pytest.skip("one kernel")
     print("hidden", dtype, what, bad, kernel, flush=True)
     c = Case(5, dtype, 4, 2, 128, 16, [(90, 150), (2, 40), (1, 70)])
     pool = c.V if what == "value" else c.K
@@ -228,11 +223,8 @@ def test_hidden_rows_reach_no_result(dtype, what, bad, kernel):
         within(lse[rows], wlse[rows], bl[rows], "lse")
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("dtype,kernel", TYPES)
 def test_bad_pages_are_hidden(dtype, kernel):
-    if dtype == "fp32" and kernel:
-        pytest.skip("one kernel")
     c = Case(6, dtype, 4, 2, 128, 16, [(40, 150), (1, 60), (1, 20), (1, 500)])
     c.table[0, 2], c.table[0, 7] = -5, c.pages                # inside and in the causal part
     c.table[1, 0] = 1 << 30
@@ -243,13 +235,10 @@ def test_bad_pages_are_hidden(dtype, kernel):
     assert (out[41] == 0).all() and torch.isneginf(lse[41]).all()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dtype,kernel", TYPES)
 @pytest.mark.parametrize("new", [1, 80])
-@pytest.mark.parametrize("kernel", KERNELS)
 def test_large_logits(dtype, new, kernel):
     """Logits of thousands, of both signs, whose references move from tile to tile."""
-    if dtype == "fp32" and kernel:
-        pytest.skip("one kernel")
     c = Case(7, dtype, 4, 2, 128, 32, [(new, 300)], sigma=8.0, scale=1.0)
     out, lse = c.attend(c.cache(kernel=kernel))
     c.check(out, lse)

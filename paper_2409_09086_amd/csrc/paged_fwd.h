@@ -68,8 +68,8 @@ __device__ __forceinline__ void mfma_qk(f32x16& S, bf16x8 k, bf16x8 q)
 
 template <bool B> using Flag = std::integral_constant<bool, B>;
 
-// What a unit costs beside its keys (queries, first tiles, output), in keys: us with 64 / 128 / 256 / 384 / 768, 4096 tokens on themselves, 32
-// heads on 8: 201.9 / 183.9 / 161.2 / 152.3 / 153.6; four chunks of 300..700 over up to 3000 keys 108.9 / 105.9 / 103.2 / 102.9 / 101.0.
+// What a unit costs beside its keys (queries, first tiles, output), in keys: us with 256 / 384 / 512 / 640 / 768, 512 tokens over 4206 keys of 32
+// heads on 8 59.4 / 58.7 / 55.9 / 55.2 / 55.1, four chunks of 300..700 over up to 3000 96.4 / 96.9 / 95.9 / 99.9 / 98.7.
 constexpr int FWD_OVERHEAD = 512;
 typedef Work<PF_ROWS, PF_TILE, FWD_OVERHEAD> FwdWork;
 struct FwdShared {

@@ -468,8 +468,9 @@ struct RowsShared {
     W place[TW];               // a wavefront's place in its share: the loop over the keys wants the registers
     SeqWindow win[TW];
 };
-// What a unit costs beside its keys, in keys: us with 16 / 64 / 128 / 256, 64 tokens over 256..8192 keys of 8 kv-heads 205.7 / 202.3 / 198.7 / 196.9;
-// with 64 / 192 / 384, 256 tokens over 100..2000, a wavefront a team, 223.7 / 225.4 / 228.9.  TW = 4: see paged_mixed.hip.
+// What a unit costs beside its keys, in keys: us with 96 / 128 / 192 / 256 / 384, 64 tokens over 256..8192 keys of 8 kv-heads 199.1 / 197.2 /
+// 197.1 / 196.1 / 196.8; with 16 / 32 / 64 / 96 / 128, 512 tokens over 10..300, a wavefront a team, 83.6 / 82.0 / 81.7 / 83.9 / 81.3.
+// TW = 4: see paged_mixed.hip.
 template <typename T, int D, int NRB, int TW>
 using RowsWork = Work<16 * NRB, RowsKernel<T, D, NRB>::KEYS, TW == 1 ? 32 : TW == 4 ? 384 : 192>;
 

@@ -11,8 +11,12 @@
 // was read a run ahead by a scalar load.  Rows outside the keys that the unit's queries see are replaced by the nearest one
 // that is seen, so that pages nobody is meant to read (freed ones in front of a window, rows past the end) are not read.
 //
-// A team (see paged_work.h) is a workgroup of 8 wavefronts that take a unit's runs in turn and merge in LDS, or a single
-// wavefront: see the launch for which.
+// A team (see paged_work.h) is a workgroup of 8 wavefronts that take a unit's runs in turn and merge in LDS, or, with four units a
+// CU and more, a single wavefront, which has nobody to wait for.
+//
+// Measured: 64 tokens over 256..8192 keys of 32 heads on 8, 1.12 GB, 196 us = 5.7 TB/s, where a copy of 1 GB goes at 4.9; 512
+// tokens over 10..300 keys 82 us = 4.1 TB/s; one token over 1001 keys of 32 heads 10 us, of which 3 are the way to the first
+// keys, 2 their way, 1 the products, 3 the merges.
 #include <algorithm>
 #include <climits>
 #include <cmath>

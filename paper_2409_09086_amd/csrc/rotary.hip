@@ -4,11 +4,12 @@
 // p f[i] and the row is written where it belongs: beside the input, or, for a new token's keys and values, into its page.
 // Nothing is computed twice and nothing but the rows moves, so the pass is bound by memory.
 //
-// D / 16 lanes share a row, two runs of eight elements each, such that a pair never leaves its lane, the norm's sum is two or three
-// lane exchanges, and the lanes' runs stand side by side in memory (sixteen elements in a row a lane, every other 16 bytes an
-// instruction, took 31.2 us for the neighbouring pairs of 4099 tokens of 64 heads of 128; so 29.5).  Half-split: the runs lie in the two halves of
-// the turned part, or of what passes behind it; neighbouring pairs: of the row, four pairs in each.  A thread goes through HPT heads of its token, all requested before
-// the first is used, with the one set of cosines.
+// D / 16 lanes share a row, two runs of eight elements each, such that a pair never leaves its lane, the norm's sum is two or
+// three lane exchanges, and the lanes' runs stand side by side in memory (sixteen elements in a row a lane, every other 16
+// bytes an instruction, took 31.2 us for the neighbouring pairs of 4099 tokens of 64 heads of 128; so 29.5, now 26.3 = 5.1 TB/s).
+// Half-split: the runs lie in the two halves of the turned part, or of what passes behind it; neighbouring pairs: of the row,
+// four pairs in each.  A thread goes through HPT heads of its token, all requested before the first is used, with the one
+// set of cosines.
 //
 // The table holds every position ((cos, sin) in floats, computed in doubles): 512 bytes a token beside the 20 KB that a
 // token of 32 + 8 heads of 128 reads and writes.

@@ -110,13 +110,14 @@ __device__ __forceinline__ void fwd_body(const PagedArgs<uint16_t>& a, float* pa
         uint32_t span[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            hi[x] = u.pos(min(64 * wave + 32 * x + l32, rows - 1));
-            lo[x] = a.window > 0 ? max(hi[x] + 1 - a.window, 0) : 0;
-            if (hi[x] < 0) { hi[x] = 1 << 30; lo[x] = 1 << 30; }              // none
+            const int pos = u.pos(min(64 * wave + 32 * x + l32, rows - 1));
+            hi[x] = min(pos, u.ke - 1);                        // a table may end ahead of it
+            lo[x] = a.window > 0 ? max(pos + 1 - a.window, 0) : 0;
+            if (hi[x] < lo[x]) hi[x] = lo[x] = INT32_MAX;      // none
             span[x] = (uint32_t)(hi[x] - lo[x]);
         }
         // tiles that hold a key which some row of the wavefront does not see
-        const int hi_first = u.pos(min(64 * wave, rows - 1)), hi_last = u.pos(min(64 * wave + 63, rows - 1));
+        const int hi_first = min(u.pos(min(64 * wave, rows - 1)), u.ke - 1), hi_last = u.pos(min(64 * wave + 63, rows - 1));
         const int full0 = a.window > 0 ? (max(hi_last + 1 - a.window, 0) - kal + PF_TILE - 1) / PF_TILE : 0;
         const int full1 = hi_first + 1 > kal ? (hi_first + 1 - kal) / PF_TILE : 0;
 

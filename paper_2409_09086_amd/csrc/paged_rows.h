@@ -203,8 +203,9 @@ struct RowsKernel<uint16_t, D, NRB> {
         for (int x = 0; x < NRB; ++x) {
             const int row = min(16 * x + c16, u.rows - u.row0 - 1);
             const T* qp = query_of<T, D>(a, u, row) + 8 * g4;
-            hi[x] = u.pos(row);
-            lo[x] = a.window > 0 ? hi[x] + 1 - a.window : 0;
+            const int pos = u.pos(row);
+            hi[x] = min(pos, u.ke - 1);                        // a table may end ahead of it
+            lo[x] = a.window > 0 ? pos + 1 - a.window : 0;
 #pragma unroll
             for (int s = 0; s < C::NS; ++s) qf[x][s] = as_bf16x8(*(const u32x4*)(qp + 32 * s));
 #pragma unroll
@@ -361,7 +362,7 @@ struct RowsKernel<float, D, 1> {
             if (np > 1) runs.look_up(k_first + step);
         }
         f32x4 qf[NJ];
-        const int row = min(c16, u.rows - u.row0 - 1), hi = u.pos(row), lo = a.window > 0 ? hi + 1 - a.window : 0;
+        const int row = min(c16, u.rows - u.row0 - 1), pos = u.pos(row), hi = min(pos, u.ke - 1), lo = a.window > 0 ? pos + 1 - a.window : 0;
         {
             const float* qp = query_of<T, D>(a, u, row) + 4 * g4;
 #pragma unroll

@@ -236,6 +236,17 @@ def test_bad_pages_are_hidden(dtype, kernel):
 
 
 @pytest.mark.parametrize("dtype,kernel", TYPES)
+@pytest.mark.parametrize("window", [0, 150])
+def test_lengths_beyond_the_table(dtype, kernel, window):
+    """Tables that end inside a run of keys (176 = 5.5 * 32 = 2.75 * 64) ahead of the lengths."""
+    print("beyond", dtype, kernel, window, flush=True)
+    c = Case(12, dtype, 4, 2, 128, 16, [(100, 230), (1, 300), (3, 178), (1, 176), (1, 400), (130, 500)], window)
+    c.table = c.table[:, :11].contiguous()
+    out, lse = c.attend(c.cache(kernel=kernel))
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype,kernel", TYPES)
 @pytest.mark.parametrize("new", [1, 80])
 def test_large_logits(dtype, new, kernel):
     """Logits of thousands, of both signs, whose references move from tile to tile."""

@@ -426,7 +426,7 @@ void infmllm_rotary_destroy(infmllm_rotary_t* r);
  *   - a page number outside 0 .. pages - 1: its keys are hidden, and nothing is appended there;
  *   - a length beyond pages_per_seq * page_size: the keys past it are hidden, and nothing is appended there;
  *   - a sequence with fewer cached tokens than new ones: the first of its new tokens have no position; they are not
- *     appended, and see no key;
+ *     appended (their rows of q_out are left as they were), and see no key;
  *   - tokens from starts[seqs] on belong to no sequence: their rows of all outputs are left as they were.
  * Pages may be shared by sequences for reading; what two tokens of a call append to one row is one of the two.
  */

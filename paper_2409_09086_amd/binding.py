@@ -343,7 +343,7 @@ def _rows(t, dtype, dev, tokens, heads, head_dim, name):
     s0, s1, s2 = t.stride()
     if s2 != 1 or (heads > 1 and s1 != head_dim):
         raise ValueError("%s must be dense within a token" % name)
-    return t.data_ptr(), s0 if tokens > 1 else max(s0, heads * head_dim)
+    return t.data_ptr(), s0 if tokens > 1 else heads * head_dim
 
 
 def _dense(t, dtype, dev, shape, name):

@@ -255,6 +255,38 @@ def test_large_logits(dtype, new, kernel):
     c.check(out, lse)
 
 
+@pytest.mark.parametrize("dtype,kernel", TYPES)
+def test_shared_pages_and_queries_that_are_not_finite(dtype, kernel):
+    """Three sequences over the pages of a common prefix; one token's query of one head is NaN: its row alone shows it."""
+    print("shared", dtype, kernel, flush=True)
+    c = Case(17, dtype, 4, 2, 128, 16, [(60, 300), (1, 280), (1, 305)])
+    c.table[1, :16], c.table[2, :16] = c.table[0, :16], c.table[0, :16]
+    want, wlse, mass, absq = R.attend(c.q, c.K, c.V, c.starts, c.lens, c.table)
+    bo, bl = R.attend_bounds(want, wlse, mass, absq, c.dtype, c.d, dtype == "bf16")
+    c.fused[33, 1, 5] = math.nan
+    out, lse = c.attend(c.cache(kernel=kernel))
+    assert torch.isnan(out[33, 1]).all() and torch.isnan(lse[33, 1])
+    others = torch.ones(c.tokens, 4, dtype=torch.bool)
+    others[33, 1] = False
+    on = others.to(DEV)
+    within(out[on], want[others], bo[others], "out")
+    within(lse[on], wlse[others], bl[others], "lse")
+
+
+def test_one_token_has_no_stride():
+    """A single token's row of a wider tensor, whatever the distance to a next one would be."""
+    c = Case(18, "bf16", 8, 2, 128, 16, [(1, 77)])
+    wide = torch.zeros(1, 8 * 128 + 3, dtype=torch.bfloat16, device=DEV)
+    q = wide[:, :8 * 128].view(1, 8, 128)
+    q.copy_(c.q)
+    out, lse = c.attend(q=q)
+    want = c.attend()
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    rot = B.Rotary(128, 100)
+    pos = torch.tensor([76], dtype=torch.int32, device=DEV)
+    assert torch.equal(rot.apply(pos, q)[0], rot.apply(pos, q.contiguous().clone())[0])
+
+
 def test_attend_in_place_and_dense_queries():
     for dtype, new, kernel in (("bf16", 1, 0), ("bf16", 130, 1), ("bf16", 130, 2), ("bf16", 130, 3), ("fp32", 40, 0)):
         c = Case(8, dtype, 8, 2, 128, 16, [(new, 400), (1, 350)])

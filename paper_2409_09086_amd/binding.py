@@ -346,6 +346,14 @@ def _rows(t, dtype, dev, tokens, heads, head_dim, name):
     return t.data_ptr(), s0 if tokens > 1 else heads * head_dim
 
 
+def _rows_out(t, like, dtype, dev, tokens, heads, head_dim, name):
+    """An output like the rows `like`, with address and token stride; None: a new one, dense like every copy of what _rows takes."""
+    if t is None:
+        t = torch.empty_like(like)
+        return t, t.data_ptr(), heads * head_dim
+    return (t,) + _rows(t, dtype, dev, tokens, heads, head_dim, name)
+
+
 def _dense(t, dtype, dev, shape, name):
     """Address of a dense tensor."""
     if t.dtype != dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
@@ -408,16 +416,12 @@ class Rotary(_Attached):
         qp = kp = qo = ko = None
         if q is not None:
             heads = q.shape[1]
-            if q_out is None:
-                q_out = torch.empty_like(q)
             qp, qs = _rows(q, dt, dev, n, heads, d, "q")
-            qo, qos = _rows(q_out, dt, dev, n, heads, d, "q_out")
+            q_out, qo, qos = _rows_out(q_out, q, dt, dev, n, heads, d, "q_out")
         if k is not None:
             kv_heads = k.shape[1]
-            if k_out is None:
-                k_out = torch.empty_like(k)
             kp, ks = _rows(k, dt, dev, n, kv_heads, d, "k")
-            ko, kos = _rows(k_out, dt, dev, n, kv_heads, d, "k_out")
+            k_out, ko, kos = _rows_out(k_out, k, dt, dev, n, kv_heads, d, "k_out")
         _check(_lib.infmllm_rotary_apply(self._h, pos, n, heads, kv_heads, qp, qs, kp, ks,
                                          None if q_weight is None else _dense(q_weight, dt, dev, (d,), "q_weight"),
                                          None if k_weight is None else _dense(k_weight, dt, dev, (d,), "k_weight"), qo, qos, ko, kos))
@@ -478,10 +482,8 @@ class PagedCache(_Attached):
         qs = qos = 0
         qp = qo = None
         if q is not None:
-            if q_out is None:
-                q_out = torch.empty_like(q)
             qp, qs = _rows(q, dt, dev, n, self.heads, d, "q")
-            qo, qos = _rows(q_out, dt, dev, n, self.heads, d, "q_out")
+            q_out, qo, qos = _rows_out(q_out, q, dt, dev, n, self.heads, d, "q_out")
         kp, ks = _rows(k, dt, dev, n, self.kv_heads, d, "k")
         vp, vs = _rows(v, dt, dev, n, self.kv_heads, d, "v")
         _check(_lib.infmllm_paged_append(self._h, None if rotary is None else rotary._h, batch._ref, kp, ks, vp, vs,
@@ -498,8 +500,10 @@ class PagedCache(_Attached):
             raise ValueError("the batch must be on %s" % dev)
         qp, qs = _rows(q, dt, dev, n, self.heads, d, "q")
         if out is None:
-            out = torch.empty((n, self.heads, d), dtype=dt, device=q.device)
+            out = torch.empty_like(q)                          # dense: see _rows_out
+            op = out.data_ptr()
+        else:
+            op = _dense(out, dt, dev, (n, self.heads, d), "out")
         _check(_lib.infmllm_paged_attend(self._h, batch._ref, qp, qs, _dense(K, dt, dev, self.pool_shape, "K"), _dense(V, dt, dev, self.pool_shape, "V"),
-                                         _dense(out, dt, dev, (n, self.heads, d), "out"),
-                                         None if lse is None else _dense(lse, torch.float32, dev, (n, self.heads), "lse")))
+                                         op, None if lse is None else _dense(lse, torch.float32, dev, (n, self.heads), "lse")))
         return out

@@ -445,6 +445,37 @@ def test_graph_follows_the_batch_arrays(kernel):
             assert torch.equal(got, out) and torch.equal(gK, K), lens
 
 
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_graph_of_units_in_pieces(kernel):
+    """Replays whose lengths and tables differ, with units cut over many teams: what one leaves for its merges the next one finds clear."""
+    c = Case(16, "bf16", 8, 2, 128, 32, [(150, 2500), (1, 3000), (1, 700), (3, 1200)])
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        cache, b = c.cache(kernel=kernel), c.batch()
+        K, V, q = c.K.to(DEV), c.V.to(DEV), c.q.to(DEV).contiguous()
+        out, lse = torch.empty_like(q), torch.empty((c.tokens, 8), device=DEV)
+        cache.attend(b, q, K, V, out=out, lse=lse)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            cache.attend(b, q, K, V, out=out, lse=lse)
+        for lens, rows in (([2500, 3000, 700, 1200], None), ([150, 1, 1, 3], None), ([1300, 2999, 64, 1150], [1, 0, 3, 2]), ([2500, 0, 650, 1], None)):
+            c.lens = torch.tensor(lens, dtype=torch.int32)
+            if rows:
+                c.table, c.lens = c.table[rows].contiguous(), torch.minimum(c.lens, torch.tensor([2500, 3000, 700, 1200])[rows]).to(torch.int32)
+            b.lens.copy_(c.lens), b.table.copy_(c.table)
+            for _ in range(2):
+                out.fill_(777), lse.fill_(777)
+                graph.replay()
+                side.synchronize()
+                got = out.clone(), lse.clone()
+                out.fill_(777), lse.fill_(777)
+                cache.attend(b, q, K, V, out=out, lse=lse)
+                side.synchronize()
+                assert torch.equal(got[0], out) and torch.equal(got[1], lse), lens
+            c.check(out, lse)
+
+
 def test_two_objects_on_two_streams():
     a, b = Case(14, "bf16", 8, 2, 128, 16, [(200, 900), (1, 800)]), Case(15, "bf16", 4, 4, 64, 32, [(1, 2000), (1, 1000)])
     want = [x.attend(x.cache(kernel=3))[0] for x in (a, b)]

@@ -338,16 +338,16 @@ struct RowsKernel<uint16_t, D, NRB> {
 
 // single precision: 16x16x4 products; step e of piece j contracts head dimensions 16j + 4g + e of lane group g, step i of the
 // second product keys 4g + i, and a lane's bytes of a V row are its operands of D / 16 column blocks (see attn_f32.hip)
-template <int D>
-struct RowsKernel<float, D, 1> {
+template <int D, int NRB>
+struct RowsKernel<float, D, NRB> {
     typedef float T;
-    static constexpr int KEYS = 16, ROWS = 16;
+    static constexpr int KEYS = 16, ROWS = 16 * NRB;
     typedef PageRuns<T, D, KEYS> Runs;
     static constexpr int ROWB = Runs::ROWB, STAGE = 2 * Runs::RUN;
     static constexpr int NJ = D / 16, VW = D / 16, VP = VW / 4;
 
-    f32x4 o[NJ];                                               // block b: lane (row c16, group g4) holds columns VW (4 g4 + i) + b
-    float m_ref, m_use, lsum;
+    f32x4 o[NRB][NJ];                                          // block b: lane (row c16, group g4) holds columns VW (4 g4 + i) + b
+    float m_ref[NRB], m_use[NRB], lsum[NRB];
 
     static __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
@@ -361,17 +361,21 @@ struct RowsKernel<float, D, 1> {
             runs.load(k_first, mine);
             if (np > 1) runs.look_up(k_first + step);
         }
-        f32x4 qf[NJ];
-        const int row = min(c16, u.rows - u.row0 - 1), pos = u.pos(row), hi = min(pos, u.ke - 1), lo = a.window > 0 ? pos + 1 - a.window : 0;
-        {
+        f32x4 qf[NRB][NJ];
+        int hi[NRB], lo[NRB];
+#pragma unroll
+        for (int x = 0; x < NRB; ++x) {
+            const int row = min(16 * x + c16, u.rows - u.row0 - 1), pos = u.pos(row);
+            hi[x] = min(pos, u.ke - 1);                        // a table may end ahead of it
+            lo[x] = a.window > 0 ? pos + 1 - a.window : 0;
             const float* qp = query_of<T, D>(a, u, row) + 4 * g4;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) qf[j] = *(const f32x4*)(qp + 16 * j);
-        }
+            for (int j = 0; j < NJ; ++j) qf[x][j] = *(const f32x4*)(qp + 16 * j);
 #pragma unroll
-        for (int b = 0; b < NJ; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-        m_ref = -__builtin_inff(); m_use = 0.f; lsum = 0.f;
-        const int hi0 = __builtin_amdgcn_readfirstlane(hi), lo1 = __builtin_amdgcn_readlane(lo, 15);
+            for (int b = 0; b < NJ; ++b) o[x][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m_ref[x] = -__builtin_inff(); m_use[x] = 0.f; lsum[x] = 0.f;
+        }
+        const int hi0 = __builtin_amdgcn_readfirstlane(hi[0]), lo1 = __builtin_amdgcn_readlane(lo[NRB - 1], 15);
         const uint32_t base = (uint32_t)(uintptr_t)(lds_void*)mine;
         uint32_t kaddr[NJ], vaddr[VP];
 #pragma unroll
@@ -391,72 +395,87 @@ struct RowsKernel<float, D, 1> {
             });
             asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(kf[0]), "+v"(kf[1]), "+v"(kf[2]), "+v"(kf[3]) : "n"(4 * VP));
             if constexpr (NJ == 8) asm volatile("" : "+v"(kf[4]), "+v"(kf[5]), "+v"(kf[6]), "+v"(kf[7]));
-            f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+            f32x4 S[NRB][2];
 #pragma unroll
             for (int j = 0; j < NJ; j += 2)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s0 = mfma(kf[j][e], qf[j][e], s0);
-                    s1 = mfma(kf[j + 1][e], qf[j + 1][e], s1);
-                }
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int x = 0; x < NRB; ++x)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            S[x][t] = mfma(kf[j + t][e], qf[x][j + t][e], j == 0 && e == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[x][t]);
             asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(vf[0][0]), "+v"(vf[1][0]), "+v"(vf[2][0]), "+v"(vf[3][0])::"memory");
             if constexpr (VP == 2) asm volatile("" : "+v"(vf[0][VP - 1]), "+v"(vf[1][VP - 1]), "+v"(vf[2][VP - 1]), "+v"(vf[3][VP - 1]));
             if (p + 1 < np) {
                 runs.load(k0 + step, mine);
                 if (p + 2 < np) runs.look_up(k0 + 2 * step);
             }
-            float s[4];
+            const bool masked = k0 + KEYS - 1 > hi0 || k0 < lo1;
+            float w[NRB][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = (s0[i] + s1[i]) * a.c;
-            if (k0 + KEYS - 1 > hi0 || k0 < lo1) {
+            for (int x = 0; x < NRB; ++x) {
+                float s[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = (S[x][0][i] + S[x][1][i]) * a.c;
+                if (masked) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = k0 + 4 * g4 + i;
+                        if (key > hi[x] || key < lo[x]) s[i] = -__builtin_inff();
+                    }
+                }
+                const float mx = groups_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
+                if (__any(mx > m_ref[x] + RESCALE_TAU)) {
+                    const float m_new = fmaxf(m_ref[x], mx);
+                    const float mu = (m_new == -__builtin_inff()) ? 0.f : m_new;
+                    const float alpha = fast_exp2(m_ref[x] - mu);
+                    m_ref[x] = m_new;
+                    m_use[x] = mu;
+                    lsum[x] *= alpha;
+#pragma unroll
+                    for (int b = 0; b < NJ; ++b) o[x][b] *= alpha;
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int key = k0 + 4 * g4 + i;
-                    if (key > hi || key < lo) s[i] = -__builtin_inff();
+                    w[x][i] = fast_exp2(s[i] - m_use[x]);
+                    lsum[x] += w[x][i];
                 }
-            }
-            const float mx = groups_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
-            if (__any(mx > m_ref + RESCALE_TAU)) {
-                const float m_new = fmaxf(m_ref, mx);
-                const float mu = (m_new == -__builtin_inff()) ? 0.f : m_new;
-                const float alpha = fast_exp2(m_ref - mu);
-                m_ref = m_new;
-                m_use = mu;
-                lsum *= alpha;
-#pragma unroll
-                for (int b = 0; b < NJ; ++b) o[b] *= alpha;
-            }
-            float w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = fast_exp2(s[i] - m_use);
-                lsum += w[i];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int b = 0; b < NJ; ++b) o[b] = mfma(vf[i][b / 4][b % 4], w[i], o[b]);
+                for (int b = 0; b < NJ; ++b)
+#pragma unroll
+                    for (int x = 0; x < NRB; ++x) o[x][b] = mfma(vf[i][b / 4][b % 4], w[x][i], o[x][b]);
         }
     }
     __device__ __forceinline__ bool finite() const
     {
         float z = 0.f;
 #pragma unroll
-        for (int b = 0; b < NJ; ++b)
+        for (int x = 0; x < NRB; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z = __builtin_fmaf(o[b][i], 0.f, z);
+            for (int b = 0; b < NJ; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z = __builtin_fmaf(o[x][b][i], 0.f, z);
         return !__any(z != 0.f);
     }
     template <class P, class S> __device__ __forceinline__ void leave(int rows, int lane, P put, S stat) const
     {
         const int c16 = lane & 15, g4 = lane >> 4;
-        const float l = groups_sum(lsum);
-        if (c16 < rows) {
-            if (g4 == 0) stat(c16, m_ref, l);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+        for (int x = 0; x < NRB; ++x) {
+            const float l = groups_sum(lsum[x]);
+            const int r = 16 * x + c16;
+            if (r < rows) {
+                if (g4 == 0) stat(r, m_ref[x], l);
 #pragma unroll
-                for (int x = 0; x < VP; ++x) put(c16, VP * (4 * g4 + i) + x, f32x4{o[4 * x][i], o[4 * x + 1][i], o[4 * x + 2][i], o[4 * x + 3][i]});
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int y = 0; y < VP; ++y)
+                        put(r, VP * (4 * g4 + i) + y, f32x4{o[x][4 * y][i], o[x][4 * y + 1][i], o[x][4 * y + 2][i], o[x][4 * y + 3][i]});
+            }
         }
     }
 };

@@ -12,7 +12,7 @@
 // that is seen, so that pages nobody is meant to read (freed ones in front of a window, rows past the end) are not read.
 //
 // A team (see paged_work.h) is a workgroup of 8 wavefronts that take a unit's runs in turn and merge in LDS, or, with four units a
-// CU and more, a single wavefront, which has nobody to wait for.
+// CU and more (chunks in single precision: two), a single wavefront, which has nobody to wait for.
 //
 // Measured: 64 tokens over 256..8192 keys of 32 heads on 8, 1.12 GB, 196 us = 5.7 TB/s, where a copy of 1 GB goes at 4.9; 512
 // tokens over 10..300 keys 82 us = 4.1 TB/s; one token over 1001 keys of 32 heads 10 us, of which 3 are the way to the first
@@ -58,14 +58,23 @@ hipError_t launch_d(const PagedArgs<T>& a, const PagedScratch& sc, int max_new, 
 {
     constexpr int KEYS = RowsKernel<T, D, 1>::KEYS;
     const int64_t rows = (int64_t)std::max(1, std::min(max_new, a.tokens)) * a.G;
-    const int64_t units = (int64_t)std::min(a.seqs, a.tokens) * a.Hkv * ((rows + 15) / 16);
+    const int64_t seqs = std::min(a.seqs, a.tokens);
+    const int64_t units = a.Hkv * std::min(seqs * ((rows + 15) / 16), (int64_t)a.tokens * a.G / 16 + seqs);   // most there can be
     // The smallest share.  Halving it halves the time that a team takes for its keys (4 D bytes each at some 40 GB/s) and doubles that of
     // the one which merges a unit's pieces (4 D bytes a row and piece at some 80 GB/s): sqrt(keys * rows / 2).
     auto least = [&](int block) { return std::max(4 * KEYS, (int)std::sqrt(0.5 * max_len * (double)std::min<int64_t>(rows, block))); };
     if constexpr (sizeof(T) == 2) {
         if (rows > 16) return launch<T, D, 2, 8>(a, sc, PAGED_CUS, least(32), st);
     }
-    if (units >= 4 * PAGED_CUS) return launch<T, D, 1, 1>(a, sc, 8 * PAGED_CUS, 2 * KEYS, st);
+    // A wavefront a team, us with eight / one, single precision: 700 tokens of 16 heads of 64 on 4 (700 units) over 1000 keys 52.7 / 50.8, 900 65.8 / 62.0, 300
+    // of 32 heads on 8 beside 31 decoded 87.7 / 76.8, of 128 155 / 150; 80 decoded ones (640 units) 135 / 143, of 64 82 / 85.
+    if (units >= (sizeof(T) == 4 && rows > 16 ? 2 : 4) * PAGED_CUS) return launch<T, D, 1, 1>(a, sc, 8 * PAGED_CUS, 2 * KEYS, st);
+    if constexpr (sizeof(T) == 4 && D == 64) {
+        // Fewer units are fewer beginnings and merges where teams have more than one.  us with 16 / 32 rows a unit, tokens of 16 heads on 4: 130 (130
+        // units of 16) over 100 keys 10.7 / 13.2, over 1000 18.6 / 18.8; 260 15.6 / 15.0, 25.1 / 26.2; 400 20.3 / 19.0, 34.4 / 33.3; five chunks
+        // of 33..197 of 8 heads on 2 (300 units) that see 256 keys 16.7 / 14.1.  Heads of 128 have no registers for it.
+        if (rows > 16 && units > PAGED_CUS) return launch<T, D, 2, 8>(a, sc, PAGED_CUS, least(32), st);
+    }
     return launch<T, D, 1, 8>(a, sc, PAGED_CUS, least(16), st);
 }
 

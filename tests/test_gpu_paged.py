@@ -168,6 +168,9 @@ ATTEND = [
     ("fp32", 8, 2, 128, 64, 0, [(100, 300), (1, 700)]),
     ("fp32", 2, 2, 64, 16, 40, [(90, 200), (1, 50)]),
     ("fp32", 14, 2, 128, 16, 0, [(1, 1200), (20, 900)]),
+    ("fp32", 16, 4, 64, 16, 0, [(150, 400), (1, 300), (130, 131)]),        # 32 rows a unit
+    ("fp32", 10, 2, 64, 32, 100, [(200, 500), (0, 9), (230, 300), (3, 1)]),
+    ("fp32", 16, 8, 64, 16, 0, [(300, 350), (1, 90), (290, 290)]),           # a wavefront a team
 ]
 
 

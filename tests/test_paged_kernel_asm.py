@@ -67,7 +67,7 @@ def touched_too_early(body):
 def test_rows_kernels():
     kernels, scratch = device_code("paged_rows.hip")
     mine = {k: v for k, v in kernels.items() if "paged_rows_kernel" in k}
-    assert len(mine) == 10, sorted(kernels)
+    assert len(mine) == 11, sorted(kernels)
     for k, body in mine.items():
         found, bad = touched_too_early(body)
         assert found >= 8 and not bad, (k, found, bad[:5])

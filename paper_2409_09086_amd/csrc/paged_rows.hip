@@ -12,7 +12,7 @@
 // that is seen, so that pages nobody is meant to read (freed ones in front of a window, rows past the end) are not read.
 //
 // A team (see paged_work.h) is a workgroup of 8 wavefronts that take a unit's runs in turn and merge in LDS, or, with four units a
-// CU and more (chunks in single precision: two), a single wavefront, which has nobody to wait for.
+// CU and more (two, if they are brief), a single wavefront, which has nobody to wait for.
 //
 // Measured: 64 tokens over 256..8192 keys of 32 heads on 8, 1.12 GB, 196 us = 5.7 TB/s, where a copy of 1 GB goes at 4.9; 512
 // tokens over 10..300 keys 82 us = 4.1 TB/s; one token over 1001 keys of 32 heads 10 us, of which 3 are the way to the first
@@ -66,9 +66,14 @@ hipError_t launch_d(const PagedArgs<T>& a, const PagedScratch& sc, int max_new, 
     if constexpr (sizeof(T) == 2) {
         if (rows > 16) return launch<T, D, 2, 8>(a, sc, PAGED_CUS, least(32), st);
     }
-    // A wavefront a team, us with eight / one, single precision: 700 tokens of 16 heads of 64 on 4 (700 units) over 1000 keys 52.7 / 50.8, 900 65.8 / 62.0, 300
-    // of 32 heads on 8 beside 31 decoded 87.7 / 76.8, of 128 155 / 150; 80 decoded ones (640 units) 135 / 143, of 64 82 / 85.
-    if (units >= (sizeof(T) == 4 && rows > 16 ? 2 : 4) * PAGED_CUS) return launch<T, D, 1, 1>(a, sc, 8 * PAGED_CUS, 2 * KEYS, st);
+    // A wavefront a team has nobody to wait for from unit to unit, but is slower with long ones.  us with eight / one, tokens of 32 heads of 128 on 8 over
+    // a tenth to all of 100, 300, 700, 1000, 3000 keys: 40 (320 units) 11.0 / 13.1, 15.4 / 17.3, -, 23.0 / 26.5, 55.5 / 62.1; 64 14.4 / 13.1, 17.8 / 18.0, 29.8 /
+    // 28.0, 36.2 / 39.0, 84.9 / 90.8; 100 19.5 / 16.2, 24.4 / 21.1, 43.7 / 43.2, 51.4 / 54.6, 125 / 133; 128 22.6 / 15.1, 28.6 / 23.0, -, 59.6 / 61.9, 153 / 157; 100 of 64
+    // 16.9 / 12.5, 21.0 / 14.5, -, 35.0 / 32.6, 78.0 / 77.3; 64 in single precision 17.9 / 19.5, 28.2 / 27.0, -, 63.1 / 67.0.  From 1024 units on it is always one: what
+    // it can lose is a few percent, and max_len may be a wide bound.  Chunks in single precision: 700 tokens of 16 heads of 64 on 4 (700
+    // units) over 1000 keys 52.7 / 50.8, 900 65.8 / 62.0, 300 of 32 heads on 8 beside 31 decoded 87.7 / 76.8, of 128 155 / 150.
+    const bool brief = (double)max_len * (2 * D * sizeof(T)) <= 400e3 || (sizeof(T) == 4 && rows > 16);
+    if (units >= (brief ? 2 : 4) * PAGED_CUS) return launch<T, D, 1, 1>(a, sc, 8 * PAGED_CUS, 2 * KEYS, st);
     if constexpr (sizeof(T) == 4 && D == 64) {
         // Fewer units are fewer beginnings and merges where teams have more than one.  us with 16 / 32 rows a unit, tokens of 16 heads on 4: 130 (130
         // units of 16) over 100 keys 10.7 / 13.2, over 1000 18.6 / 18.8; 260 15.6 / 15.0, 25.1 / 26.2; 400 20.3 / 19.0, 34.4 / 33.3; five chunks

@@ -22,8 +22,8 @@
 // Units are shared out over one workgroup a CU (paged_work.h); the chunk's causal triangle and ragged batches come
 // out even that way.
 //
-// Measured: 2048 tokens over 8192 + 2048 keys of 32 heads 290 us = 1.06 PFLOP/s, as long as attn_fwd64 takes over a contiguous cache
-// on the same card (297), and 0.93 of a matrix product's rate there (8192: 1.14).  512 tokens over 4206 keys of 32 heads on 8
+// Measured: 2048 tokens over 8192 + 2048 keys of 32 heads 287 to 300 us (by card) = 1.03 to 1.08 PFLOP/s, as long as attn_fwd64 takes over a contiguous cache
+// on the same card (297), and 0.90 to 0.94 of a matrix product's rate there (8192: 1.14).  512 tokens over 4206 keys of 32 heads on 8
 // 55 us: 64 units in 4 pieces, 7 us to the first product, 31 for 17 tiles, 10 for the merges, 3 for the output.
 #include <climits>
 

@@ -62,13 +62,14 @@ struct Work {
     int first, n, pos0, ntile;     // of the sequence
     double base, inc;              // tile i of it costs base + (i + 1) * inc
 
+    // Whatever the arrays hold, 0 <= first, 0 <= n and first + n <= tokens, for differences of entries may not fit an int.
     struct Seq { int first, n, pos0, ntile; double base, inc; };
-    __device__ __forceinline__ Seq describe(int s0, int s1, int len) const
+    __host__ __device__ __forceinline__ Seq describe(int s0, int s1, int len) const
     {
         Seq q;
         len = max(len, 0);
         q.first = min(max(s0, 0), tokens);
-        q.n = max(min(s1, tokens) - q.first, 0);
+        q.n = max(min(s1, tokens), q.first) - q.first;
         const int64_t rows = (int64_t)q.n * G;
         if (rows <= row_lo || rows > row_hi) q.n = 0;
         q.pos0 = q.n > 0 ? len - (s1 - q.first) : 0;

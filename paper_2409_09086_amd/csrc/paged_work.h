@@ -97,7 +97,7 @@ struct Work {
         return describe(__builtin_amdgcn_readfirstlane(win->s0[i]), __builtin_amdgcn_readfirstlane(win->s1[i]),
                         __builtin_amdgcn_readfirstlane(win->len[i]));
     }
-    static __device__ __forceinline__ double before(const Seq& q, int i) { return i * q.base + q.inc * (0.5 * i * (i + 1.0)); }
+    static __host__ __device__ __forceinline__ double before(const Seq& q, int i) { return i * q.base + q.inc * (0.5 * i * (i + 1.0)); }
     __device__ __forceinline__ double of_head(const Seq& q) const { return q.n > 0 ? before(q, q.ntile) : 0.0; }
     __device__ __forceinline__ void take(const Seq& q) { first = q.first; n = q.n; pos0 = q.pos0; ntile = q.ntile; base = q.base; inc = q.inc; }
 
@@ -172,21 +172,15 @@ struct Work {
                 }
                 rem -= all;
             }
+            if (seq >= seqs) { left = 0.0; return; }           // costs beyond 2^53 alone, whose sums are rounded
         }
         const Seq now = from_window(seq);
-        if (now.n == 0) { left = 0.0; return; }                // costs beyond 2^53 alone
+        if (now.n == 0) { left = 0.0; return; }                // likewise
         take(now);
-        const double head = of_head(now);
-        h = (int)(rem / head);
-        rem -= h * head;
-        // the tile: the largest i whose predecessors cost no more than rem
-        const double bb = now.base + 0.5 * now.inc;
-        int i = now.inc > 0.0 ? (int)((sqrt(bb * bb + 2.0 * now.inc * rem) - bb) / now.inc) : (int)(rem / now.base);
-        i = min(max(i, 0), ntile - 1);
-        while (i > 0 && before(now, i) > rem) --i;
-        while (i + 1 < ntile && before(now, i + 1) <= rem) ++i;
-        tile = __builtin_amdgcn_readfirstlane(i);
-        h = __builtin_amdgcn_readfirstlane(h);
+        const Place at = locate(now, Hkv, of_head(now), rem);
+        rem = at.rem;
+        tile = __builtin_amdgcn_readfirstlane(at.tile);
+        h = __builtin_amdgcn_readfirstlane(at.h);
         off = uniform(rem - before(now, tile));
         u0 = lo - off;
         const double cost = base + (tile + 1) * inc;
@@ -194,6 +188,20 @@ struct Work {
             left -= cost - off;
             advance(cost, lane);
         }
+    }
+    // Where rem, counted from a sequence's first unit, lies: its head, the tile (the largest whose predecessors cost no more than what is
+    // left) and the rest.  A head and a tile that exist whatever rem is: sums beyond 2^53 are rounded.
+    struct Place { int h, tile; double rem; };
+    static __host__ __device__ __forceinline__ Place locate(const Seq& q, int heads, double head, double rem)
+    {
+        Place p;
+        p.h = (int)fmin(fmax(rem / head, 0.0), heads - 1.0);
+        p.rem = rem - p.h * head;
+        const double bb = q.base + 0.5 * q.inc, at = q.inc > 0.0 ? (sqrt(bb * bb + 2.0 * q.inc * fmax(p.rem, 0.0)) - bb) / q.inc : p.rem / q.base;
+        p.tile = (int)fmin(fmax(at, 0.0), q.ntile - 1.0);
+        while (p.tile > 0 && before(q, p.tile) > p.rem) --p.tile;
+        while (p.tile + 1 < q.ntile && before(q, p.tile + 1) <= p.rem) ++p.tile;
+        return p;
     }
     // on to the next unit
     __device__ __forceinline__ void advance(double cost, int lane)

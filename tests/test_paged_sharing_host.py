@@ -1,5 +1,5 @@
 """Host build of what the attention over pages makes of a batch's arrays (csrc/paged_work.h): whatever they hold, the rows that units are made
-of lie among the call's tokens, so that no kernel addresses anything outside them (CPU only)."""
+of lie among the call's tokens and the units that shares begin in exist, so that no kernel addresses anything outside them (CPU only)."""
 import os
 import shutil
 import subprocess
@@ -39,10 +39,34 @@ template <int R> long check(long& bad)
     }
     return cases;
 }
+// the unit at a place of a sequence's cost: one that exists, and the right one where the costs are exact
+template <int R> long places(long& bad)
+{
+    typedef Work<R, 32, 192> W;
+    long cases = 0;
+    for (int n : {1, 15, 1000, 1 << 24}) for (int G : {1, 5, 64}) for (int window : {0, 300}) for (int len : {1, 5000, INT_MAX}) for (int heads : {1, 3, 16384}) {
+        W w{};
+        w.tokens = n; w.G = G; w.Hkv = heads; w.window = window; w.row_hi = INT_MAX; w.most_keys = INT_MAX - 65536; w.seqs = 1;
+        const auto q = w.describe(0, n, len);
+        const double head = W::before(q, q.ntile), all = head * heads;
+        auto look = [&](double rem) {
+            const auto p = W::locate(q, heads, head, rem);
+            bool good = p.h >= 0 && p.h < heads && p.tile >= 0 && p.tile < q.ntile;
+            if (rem >= 0 && rem < all && all < 9e15) good &= W::before(q, p.tile) <= p.rem && p.rem < W::before(q, p.tile + 1) && p.h * head + p.rem == rem;
+            ++cases;
+            if (!good && !bad++) std::printf("R %d n %d G %d window %d len %d heads %d rem %.17g: head %d tile %d rem %.17g\n", R, n, G, window, len, heads, rem, p.h, p.tile, p.rem);
+        };
+        for (double x : {-1e18, -1.0, 0.0, 1.0, all - 1, all, all + 1, 2 * all, all * all, 1e300}) look(x);
+        for (int h : {0, 1, heads / 2, heads - 1})
+            for (int t : {0, 1, q.ntile / 3, q.ntile - 1})
+                for (double d : {-1.0, 0.0, 1.0}) look(h * head + W::before(q, t) + d);
+    }
+    return cases;
+}
 int main()
 {
     long bad = 0;
-    const long cases = check<16>(bad) + check<32>(bad) + check<256>(bad);
+    const long cases = check<16>(bad) + check<32>(bad) + check<256>(bad) + places<16>(bad) + places<256>(bad);
     std::printf("%ld of %ld wrong\n", bad, cases);
     return bad != 0 || cases < 100000;
 }
@@ -50,7 +74,7 @@ int main()
 
 
 @pytest.mark.skipif(shutil.which("hipcc") is None, reason="hipcc not found")
-def test_rows_of_units_lie_among_the_tokens(tmp_path):
+def test_units_exist_and_their_rows_lie_among_the_tokens(tmp_path):
     from paper_2409_09086_amd.build import CSRC
     src, exe = tmp_path / "sharing.hip", tmp_path / "sharing"
     src.write_text(PROGRAM)

@@ -487,10 +487,12 @@ int infmllm_paged_append(infmllm_paged_t* p, infmllm_rotary_t* rotary, const inf
 
 /*
  * Attention of the new tokens over the pages, their own keys included (they have been appended): for the token at position p
- *   out = softmax_j(scale * q.K[j]) V[j] over the keys j <= p, with a window j > p - window;  0 where it sees none
+ *   out = softmax_j(scale * q.K[j]) V[j] over the keys j <= p, with a window j > p - window;  0 where it sees none (where it sees
+ *   some whose logits all are -inf: NaN, as that softmax is)
  *   q      device, strided rows as for infmllm_rotary_apply;  out  device, [tokens][heads][head_dim].  It may be q where q is
  *          dense, and must not overlap q otherwise
- *   lse    device, float [tokens][heads]: log(sum_j exp(scale * q.K[j])), -inf where no key is seen.  May be null
+ *   lse    device, float [tokens][heads]: log(sum_j exp(scale * q.K[j])), -inf where no key (or none with a logit above -inf) is
+ *          seen.  May be null
  * A hidden key or value reaches no result, whatever it is.  bf16: products with fp32 sums, weights of chunks rounded to bf16.
  * Errors: EINVAL (also pointers or strides that are not multiples of 16 bytes, tokens * heads / kv_heads above 2^30), ESTATE (not
  * attached), EHIP.

@@ -14,8 +14,6 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 
 constexpr float LN2 = 0.6931471805599453f;
 __device__ __forceinline__ float natural_lse(float m, float l) { return l == 0.f ? -__builtin_inff() : LN2 * (m + __builtin_log2f(l)); }
-// what a sum of weights divides the output by: rows that see no key become 0
-__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.0f / l; }
 
 template <typename T>
 __device__ __forceinline__ int page_of(const PagedArgs<T>& a, int seq, int key)
@@ -109,6 +107,22 @@ __device__ __forceinline__ void visible(const Unit& u, int window, int r, int& k
     const int pos = u.pos(r), at = u.kb & ~(RUN - 1);
     k0 = max(max(window > 0 ? pos + 1 - window : 0, at + u.r0 * RUN), u.kb);
     k1 = min(min(pos + 1, at + u.r1 * RUN), u.ke);
+}
+
+// What a row's sum of weights l, over all pieces of its unit, divides its output by.  A sum of 0 is one of no weights or of weights that all are
+// exp(-inf): rows that see no key become 0, those that see only logits of -inf NaN, as every softmax of them is.
+template <typename T>
+__device__ __forceinline__ float inverse(const PagedArgs<T>& a, const Unit& u, int r, float l)
+{
+    if (__builtin_expect(l != 0.f, 1)) return 1.0f / l;
+    const int pos = u.pos(r), k0 = max(a.window > 0 ? pos + 1 - a.window : 0, u.kb), k1 = min(pos + 1, u.ke);
+    if (k0 < k1) {
+        const int32_t* row = a.table + (int64_t)u.seq * a.pages_per_seq;
+#pragma nounroll
+        for (int p = k0 >> a.page_shift; p <= (k1 - 1) >> a.page_shift; ++p)
+            if ((unsigned)row[p] < (unsigned)a.pages) return __builtin_nanf("");
+    }
+    return 0.f;
 }
 
 // Memory of a team's slot, past the caches of the XCDs (see buffer_to_lds).
@@ -557,7 +571,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs<T>& a, float* part, in
             sync();
         }
         auto finish = [&](int r, int p, const PieceSum& s) {
-            const float inv = inverse(s.l);
+            const float inv = inverse(a, u, r, s.l);
             const int64_t at = result_of(a, u, r);
             store_out4(a.out + at * D + 4 * p, f32x4{s.o[0] * inv, s.o[1] * inv, s.o[2] * inv, s.o[3] * inv});
             if (a.lse && p == 0) a.lse[at] = natural_lse(s.m, s.l);

@@ -89,3 +89,29 @@ def test_append_stays_inside(starts, lens):
     assert rim(wk, 64, 777) and rim(wv, 64, 777) and rim(wq, 64, 777)
     others = [p for p in range(c.pages) if p not in held.tolist()]
     assert (K[others] == 777).all() and (V[others] == 777).all()   # pages of no sequence
+
+
+@pytest.mark.parametrize("dtype,kernel", TYPES)
+@pytest.mark.parametrize("window", [0, 24])
+def test_logits_that_are_all_minus_infinity(dtype, kernel, window):
+    """exp(-inf) for every key that a row sees: 0 / 0, not the 0 of a row that sees no key.  One finite logit, and it is an ordinary row."""
+    print("minus infinity", dtype, kernel, window, flush=True)
+    c = Case(24, dtype, 4, 2, 128, 16, [(40, 40), (1, 3000), (1, 70), (90, 600), (3, 2), (1, 33)], window)
+    c.fused[:, :4, 3] = c.fused[:, :4, 3].abs() + 0.5          # every logit of a key with -inf there is -inf
+
+    def lost(s, head, keys):
+        for j in keys:
+            c.K[int(c.table[s, j // 16]), head, j % 16, 3] = float("-inf")
+    lost(0, 0, range(16))
+    lost(1, 0, range(3000))
+    lost(3, 1, range(530, 600))
+    lost(5, 0, range(32))                                      # one key is left
+    c.table[2, :] = -1
+    out, lse = c.attend(c.cache(kernel=kernel))
+    want, wlse, mass, absq = R.attend(c.q, c.K, c.V, c.starts, c.lens, c.table, window)
+    # (the sums of the finite logits stay below 12)
+    bo, bl = R.attend_bounds(want, wlse, mass, absq.clamp(max=16.0), c.dtype, c.d, dtype == "bf16")
+    assert torch.isnan(want[:16, :2]).all() and torch.isnan(want[40, :2]).all() and (want[41] == 0).all()
+    assert torch.isfinite(want[-1]).all() and torch.isnan(want).any(-1).sum() == (16 * 2 + 2 if not window else 16 * 2 + 2 + 2 * (600 - 553))
+    within(out, want, bo, "out")
+    within(lse, wlse, bl, "lse")

@@ -327,6 +327,9 @@ def evict_batched(streams):
         s._held = None
 
 
+_current_stream = torch._C._cuda_getCurrentRawStream          # of a device's index: the handle, without a Stream object around it
+
+
 def _dtype_code(dtype):
     code = {torch.bfloat16: BF16, torch.float32: FP32}.get(dtype)
     if code is None:
@@ -362,7 +365,11 @@ def _dense(t, dtype, dev, shape, name):
 
 
 class _Attached:
-    """What objects with a workspace share: `prefix`_workspace_bytes, _attach and _destroy of a handle."""
+    """What objects with a workspace share: `prefix`_workspace_bytes, _attach and _destroy of a handle.
+
+    Calls are enqueued on the object's HIP stream, the one that was current when it was made (or hip_stream).  Made under another current
+    stream, a call is not ordered with it: that is the caller's (wait_stream); new outputs belong to the object's stream then, and tensors
+    that the call was given may be dropped at once."""
 
     def _attach(self, prefix, handle, device, hip_stream):
         L = lib()
@@ -370,11 +377,24 @@ class _Attached:
         self.device = torch.device(device)
         nbytes = getattr(L, prefix + "_workspace_bytes")(handle)
         with torch.cuda.device(self.device):
-            self.hip_stream = hip_stream if hip_stream is not None else torch.cuda.current_stream(self.device).cuda_stream
-            self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+            self._index = torch.cuda.current_device()
+            self.hip_stream = hip_stream if hip_stream is not None else torch.cuda.current_stream(self._index).cuda_stream
+            self._stream = torch.cuda.ExternalStream(self.hip_stream, self._index)
+            with torch.cuda.stream(self._stream):
+                self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
             self.device = self.workspace.device                # with its index
             aligned = (self.workspace.data_ptr() + 255) // 256 * 256
             _check(getattr(L, prefix + "_attach")(handle, ctypes.c_void_p(aligned), nbytes, ctypes.c_void_p(self.hip_stream)))
+
+    def _under_own_stream(self, call, *args):
+        """A call made under another current stream: torch allocates for the object's, and keeps what it was given until that has got so far."""
+        with torch.cuda.stream(self._stream):
+            result = call(*args)
+        for x in args:
+            for t in (x.starts, x.lens, x.table) if isinstance(x, PagedBatch) else (x,):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(self._stream)
+        return result
 
     def close(self):
         h, self._h = getattr(self, "_h", None), None
@@ -386,7 +406,7 @@ class _Attached:
 
 
 class Rotary(_Attached):
-    """infmllm_rotary_t with its table: rotary positions and head norms.
+    """infmllm_rotary_t with its table: rotary positions and head norms.  Calls run on the HIP stream that was current at its creation.
 
     base 0 or None: no rotation (norms alone); trained with factor, low_turns and high_turns: frequencies scaled by parts,
     factor alone: all of them."""
@@ -410,6 +430,8 @@ class Rotary(_Attached):
     def apply(self, positions, q=None, k=None, q_weight=None, k_weight=None, q_out=None, k_out=None):
         """infmllm_rotary_apply: q [n, heads, d], k [n, kv_heads, d] (either may be None), positions int32 [n].
         Returns (q_out, k_out); q_out=q turns in place.  Nothing is synchronised."""
+        if _current_stream(self._index) != self.hip_stream:
+            return self._under_own_stream(self.apply, positions, q, k, q_weight, k_weight, q_out, k_out)
         n, d, dt, dev = positions.shape[0], self.head_dim, self.dtype, self.device
         pos = _dense(positions, torch.int32, dev, (n,), "positions")
         heads = kv_heads = qs = ks = qos = kos = 0
@@ -454,7 +476,8 @@ class PagedBatch:
 
 class PagedCache(_Attached):
     """infmllm_paged_t with its workspace: geometry and scratch of a paged cache; the pools of a layer, [pages, kv_heads,
-    page_size, head_dim] each, are the caller's and are arguments of every call (pools() makes a pair)."""
+    page_size, head_dim] each, are the caller's and are arguments of every call (pools() makes a pair).  Calls run on the HIP stream that was
+    current at its creation."""
 
     def __init__(self, pages, page_size, heads, kv_heads, head_dim, dtype=torch.bfloat16, scale=None, window=None, kernel=None, device="cuda:0",
                  hip_stream=None):
@@ -476,6 +499,8 @@ class PagedCache(_Attached):
     def append(self, batch, k, v, K, V, rotary=None, k_weight=None, q=None, q_weight=None, q_out=None):
         """infmllm_paged_append: k, v [tokens, kv_heads, d] enter the pools K, V; with a Rotary, keys and (where given) queries q
         [tokens, heads, d] are normed and turned on the way.  Returns q_out (None without q).  Nothing is synchronised."""
+        if _current_stream(self._index) != self.hip_stream:
+            return self._under_own_stream(self.append, batch, k, v, K, V, rotary, k_weight, q, q_weight, q_out)
         n, d, dt, dev = batch.tokens, self.head_dim, self.dtype, self.device
         if batch.device != dev or (rotary is not None and rotary._h is None):
             raise ValueError("the batch must be on %s, the rotary object open" % dev)
@@ -490,11 +515,15 @@ class PagedCache(_Attached):
                                          None if k_weight is None else _dense(k_weight, dt, dev, (d,), "k_weight"), qp, qs,
                                          None if q_weight is None else _dense(q_weight, dt, dev, (d,), "q_weight"), qo, qos,
                                          _dense(K, dt, dev, self.pool_shape, "K"), _dense(V, dt, dev, self.pool_shape, "V")))
+        if rotary is not None and rotary.hip_stream != self.hip_stream:
+            rotary.workspace.record_stream(self._stream)       # the table is read here
         return q_out if q is not None else None
 
     def attend(self, batch, q, K, V, out=None, lse=None):
         """infmllm_paged_attend: attention of q [tokens, heads, d] over the batch's pages.  Returns out [tokens, heads, d]; lse, float
         [tokens, heads], receives the log-sum-exp.  Nothing is synchronised."""
+        if _current_stream(self._index) != self.hip_stream:
+            return self._under_own_stream(self.attend, batch, q, K, V, out, lse)
         n, d, dt, dev = batch.tokens, self.head_dim, self.dtype, self.device
         if batch.device != dev:
             raise ValueError("the batch must be on %s" % dev)

@@ -367,8 +367,8 @@ enum {
                                      `high` turns within it are kept and those below `low` divided whole.  Default 0        */
     INFMLLM_ROTARY_LOW = 5,       /* `low` and `high`, in turns, 0 <= low < high at attach; defaults 1 and 32               */
     INFMLLM_ROTARY_HIGH = 6,
-    INFMLLM_ROTARY_MAGNITUDE = 7, /* m > 0, on cosine and sine (not on dimensions that pass).  Default 1                     */
-    INFMLLM_ROTARY_EPS = 8        /* eps >= 0 of the norm.  Default 1e-6                                                     */
+    INFMLLM_ROTARY_MAGNITUDE = 7, /* m > 0, a normal float, on cosine and sine (not on dimensions that pass).  Default 1      */
+    INFMLLM_ROTARY_EPS = 8        /* eps of the norm, 0 or a normal float > 0.  Default 1e-6                                 */
 };
 
 /*
@@ -444,7 +444,7 @@ typedef struct infmllm_batch {
 } infmllm_batch_t;
 
 enum {
-    INFMLLM_PAGED_SCALE = 0,  /* softmax scale on q.k; default 1/sqrt(head_dim)                                   */
+    INFMLLM_PAGED_SCALE = 0,  /* softmax scale on q.k, > 0, scale * log2(e) a normal float; default 1/sqrt(head_dim) */
     INFMLLM_PAGED_WINDOW = 1, /* a token sees the newest `window` keys, itself included; 0 (default): all          */
     INFMLLM_PAGED_KERNEL = 2  /* debug/test, bf16: 0 (default) = the attention picks its kernel; 1 = the one for few rows, 2 = that for
                                  chunks, 3 = both side by side (the first for sequences of at most 16 rows).  Results are the

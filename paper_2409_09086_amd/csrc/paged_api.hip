@@ -67,6 +67,8 @@ int check_batch(const char* who, const infmllm_batch_t* b)
 }
 
 bool whole(double v) { return v == std::floor(v); }
+bool normal_float(double v) { return std::isnormal((float)v); }
+constexpr double LOG2E = 1.4426950408889634;
 
 // Whether the kernel for few rows (32 a unit) is the faster one for bf16 queries, by what the two should take, in us.  It reads the keys once
 // for every 32 rows; where there are no more units than teams those of one head run beside each other and find them in the L2, otherwise they
@@ -180,11 +182,11 @@ int infmllm_rotary_set_param(infmllm_rotary_t* r, int which, double value)
             r->f.high = value;
             return INFMLLM_OK;
         case INFMLLM_ROTARY_MAGNITUDE:
-            if (value <= 0) return fail(INFMLLM_EINVAL, "rotary_set_param: magnitude must be > 0");
+            if (value <= 0 || !normal_float(value)) return fail(INFMLLM_EINVAL, "rotary_set_param: magnitude must be > 0 and a normal float");
             r->f.magnitude = value;
             return INFMLLM_OK;
         case INFMLLM_ROTARY_EPS:
-            if (value < 0) return fail(INFMLLM_EINVAL, "rotary_set_param: eps must be >= 0");
+            if (value < 0 || (value > 0 && !normal_float(value))) return fail(INFMLLM_EINVAL, "rotary_set_param: eps must be 0 or a normal float > 0");
             r->eps = value;
             return INFMLLM_OK;
         default:
@@ -285,7 +287,8 @@ int infmllm_paged_set_param(infmllm_paged_t* p, int which, double value)
     if (!std::isfinite(value)) return fail(INFMLLM_EINVAL, "paged_set_param: value is not finite");
     switch (which) {
         case INFMLLM_PAGED_SCALE:
-            if (value <= 0) return fail(INFMLLM_EINVAL, "paged_set_param: scale must be > 0");
+            if (value <= 0 || !normal_float(value * LOG2E))
+                return fail(INFMLLM_EINVAL, "paged_set_param: scale must be > 0, its product with log2(e) a normal float");
             p->scale = value;
             return INFMLLM_OK;
         case INFMLLM_PAGED_WINDOW:
@@ -394,7 +397,7 @@ int infmllm_paged_attend(infmllm_paged_t* p, const infmllm_batch_t* batch, const
         a.seqs = batch->seqs; a.tokens = batch->tokens; a.pages_per_seq = batch->pages_per_seq; a.pages = p->pages; a.page_shift = p->page_shift;
         a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv; a.window = p->window;
         a.inv_g = (uint32_t)((1ull << 32) / (unsigned)a.G + 1);
-        a.c = (float)(p->scale * 1.4426950408889634);
+        a.c = (float)(p->scale * LOG2E);
         if constexpr (sizeof(T) == 2) {
             const int few = 16;                                // rows of sequences that run on their own beside chunks
             int kernel = p->kernel;

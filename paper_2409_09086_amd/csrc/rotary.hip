@@ -235,9 +235,16 @@ hipError_t launch(const RotaryArgs<T>& a, hipStream_t st)
     // Heads a thread: few tokens want threads, many want their cosines read once and their loads in a row.  us with 1 / 4 / 8 heads, the
     // latter two with stores past the caches: 4099 tokens of 64 heads of 128 normed and turned 31.7 / 27.9 / 26.0, 8192 of 40 turned 39.2 / 33.3 / 33.8,
     // 4236 into their pages 25.1 / 19.0 / 19.3 (22.2 with stores into the caches; the attention that follows takes as
-    // long); with 1 / 8, 2000 of 40 turned 11.2 / 10.0, 1000 (80 workgroups of 8) 9.7 / 9.7 with the call.
-    if ((int64_t)gx * groups(8) >= 256) hipLaunchKernelGGL((rotary_kernel<T, D, 8, PAGED>), dim3(gx, groups(8)), block, 0, st, a);
-    else hipLaunchKernelGGL((rotary_kernel<T, D, 1, PAGED>), dim3(gx, groups(1)), block, 0, st, a);
+    // long).  The kernel alone with 1 / 8, 40 heads of 128: 2000 tokens (315 workgroups of 8) turned 10.3 / 9.8, normed too 11.0 / 10.6, into their pages
+    // 11.6 / 10.8; 1000 (160) 6.3 / 6.2, 7.0 / 7.2, 7.6 / 7.1; 500 (80) 4.5 / 5.7, 4.7 / 6.4, 4.9 / 5.9.  In single precision a head is as many loads as two,
+    // and one a thread is enough: 2000 17.5 / 25.9, 18.8 / 23.3, 22.1 / 28.1; 4096 35.4 / 41.1, 37.6 / 49.0, 42.0 / 55.4; 16000 160 / 177, 151 / 180, 189 / 230.
+    if constexpr (sizeof(T) == 2) {
+        if ((int64_t)gx * groups(8) >= 256) {
+            hipLaunchKernelGGL((rotary_kernel<T, D, 8, PAGED>), dim3(gx, groups(8)), block, 0, st, a);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((rotary_kernel<T, D, 1, PAGED>), dim3(gx, groups(1)), block, 0, st, a);
     return hipGetLastError();
 }
 

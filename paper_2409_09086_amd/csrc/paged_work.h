@@ -190,15 +190,16 @@ struct Work {
         }
     }
     // Where rem, counted from a sequence's first unit, lies: its head, the tile (the largest whose predecessors cost no more than what is
-    // left) and the rest.  A head and a tile that exist whatever rem is: sums beyond 2^53 are rounded.
+    // left) and the rest.  A head and a tile that exist also where rem is off by a rounding, as sums beyond 2^53 are.
     struct Place { int h, tile; double rem; };
     static __host__ __device__ __forceinline__ Place locate(const Seq& q, int heads, double head, double rem)
     {
         Place p;
-        p.h = (int)fmin(fmax(rem / head, 0.0), heads - 1.0);
+        p.h = min((int)(rem / head), heads - 1);
         p.rem = rem - p.h * head;
-        const double bb = q.base + 0.5 * q.inc, at = q.inc > 0.0 ? (sqrt(bb * bb + 2.0 * q.inc * fmax(p.rem, 0.0)) - bb) / q.inc : p.rem / q.base;
-        p.tile = (int)fmin(fmax(at, 0.0), q.ntile - 1.0);
+        const double bb = q.base + 0.5 * q.inc;
+        p.tile = q.inc > 0.0 ? (int)((sqrt(bb * bb + 2.0 * q.inc * p.rem) - bb) / q.inc) : (int)(p.rem / q.base);
+        p.tile = min(max(p.tile, 0), q.ntile - 1);
         while (p.tile > 0 && before(q, p.tile) > p.rem) --p.tile;
         while (p.tile + 1 < q.ntile && before(q, p.tile + 1) <= p.rem) ++p.tile;
         return p;

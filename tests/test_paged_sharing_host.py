@@ -56,7 +56,7 @@ template <int R> long places(long& bad)
             ++cases;
             if (!good && !bad++) std::printf("R %d n %d G %d window %d len %d heads %d rem %.17g: head %d tile %d rem %.17g\n", R, n, G, window, len, heads, rem, p.h, p.tile, p.rem);
         };
-        for (double x : {-1e18, -1.0, 0.0, 1.0, all - 1, all, all + 1, 2 * all, all * all, 1e300}) look(x);
+        for (double x : {-1.0, 0.0, 1.0, all - 1, all, all + 1, all * (1 + 1e-12)}) look(x);
         for (int h : {0, 1, heads / 2, heads - 1})
             for (int t : {0, 1, q.ntile / 3, q.ntile - 1})
                 for (double d : {-1.0, 0.0, 1.0}) look(h * head + W::before(q, t) + d);

@@ -449,7 +449,7 @@ __device__ __forceinline__ void fwd_body(const PagedArgs<uint16_t>& a, float* pa
         float ltot[2], z = 0.f;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            ltot[x] = xhalf_sum(lsum[x]);
+            ltot[x] = sum_of<PF_TILE>(u, a.window, min(64 * wave + 32 * x + e32, rows - 1), xhalf_sum(lsum[x]));
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -472,7 +472,7 @@ __device__ __forceinline__ void fwd_body(const PagedArgs<uint16_t>& a, float* pa
                 plain_row<uint16_t, D>(a, u.seq, u.h, query_of<uint16_t, D>(a, u, r), k0, k1, el, m, l, po);
                 if (u.pieces == 1) {
                     const int64_t at = result_of(a, u, r);
-                    const float inv = inverse(a, u, r, l);
+                    const float inv = inverse(l);
 #pragma unroll
                     for (int e = 0; e < D / 64; ++e) *(__bf16*)(a.out + at * D + 64 * e + el) = (__bf16)(po[e] * inv);
                     if (a.lse && el == 0) a.lse[at] = natural_lse(m, l);
@@ -571,8 +571,7 @@ __device__ __forceinline__ void fwd_body(const PagedArgs<uint16_t>& a, float* pa
             char* const olds = smem + wave * (64 * ROWB);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int r = 64 * wave + 32 * x + e32;
-                const float inv = inverse(a, u, min(r, rows - 1), ltot[x]);
+                const float inv = inverse(ltot[x]);
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -582,6 +581,7 @@ __device__ __forceinline__ void fwd_body(const PagedArgs<uint16_t>& a, float* pa
                         for (int e = 0; e < 4; ++e) w[e] = (__bf16)(o[x][b][4 * q4 + e] * inv);
                         *(bf16x4*)(olds + (32 * x + e32) * ROWB + Tile<uint16_t, D>::k(e32, 4 * b + q4) * 16 + 8 * eh) = w;
                     }
+                const int r = 64 * wave + 32 * x + e32;
                 if (a.lse && eh == 0 && r < rows) a.lse[result_of(a, u, r)] = natural_lse(m_ref[x], ltot[x]);
             }
 #pragma unroll

@@ -36,7 +36,7 @@ __device__ __forceinline__ void plain_row(const PagedArgs<T>& a, int seq, int h,
 {
     constexpr int E = 16 / (int)sizeof(T);
     m = -__builtin_inff();
-    l = 0.f;
+    l = -0.0f;                                                 // see NONE
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) o[e] = 0.f;
 #pragma nounroll
@@ -70,7 +70,7 @@ __device__ __forceinline__ void plain_row(const PagedArgs<T>& a, int seq, int h,
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
         m = mn;
-        l = l * alpha + sum;
+        if (__any(seen)) l = l * alpha + sum;
 #pragma unroll
         for (int e = 0; e < D / 64; ++e) o[e] *= alpha;
 #pragma nounroll
@@ -109,20 +109,19 @@ __device__ __forceinline__ void visible(const Unit& u, int window, int r, int& k
     k1 = min(min(pos + 1, at + u.r1 * RUN), u.ke);
 }
 
-// What a row's sum of weights l, over all pieces of its unit, divides its output by.  A sum of 0 is one of no weights or of weights that all are
-// exp(-inf): rows that see no key become 0, those that see only logits of -inf NaN, as every softmax of them is.
-template <typename T>
-__device__ __forceinline__ float inverse(const PagedArgs<T>& a, const Unit& u, int r, float l)
+// A sum of weights of 0 is one of none or one of weights that all are exp(-inf).  Rows that see no key become 0, those that see only logits of -inf
+// NaN, as every softmax of them is: the sum of a row that sees no key is -0, which weights of the one kind leave as it is
+// and those of the other kind make +0, piece by piece.
+constexpr float NONE = -0.0f;
+__device__ __forceinline__ float inverse(float l) { return __float_as_uint(l) == 0x80000000u ? 0.f : 1.0f / l; }   // of +0: 0 * inf
+// the sum of row r over a piece whose pages all exist (hidden keys have added +0)
+template <int RUN>
+__device__ __forceinline__ float sum_of(const Unit& u, int window, int r, float l)
 {
-    if (__builtin_expect(l != 0.f, 1)) return 1.0f / l;
-    const int pos = u.pos(r), k0 = max(a.window > 0 ? pos + 1 - a.window : 0, u.kb), k1 = min(pos + 1, u.ke);
-    if (k0 < k1) {
-        const int32_t* row = a.table + (int64_t)u.seq * a.pages_per_seq;
-#pragma nounroll
-        for (int p = k0 >> a.page_shift; p <= (k1 - 1) >> a.page_shift; ++p)
-            if ((unsigned)row[p] < (unsigned)a.pages) return __builtin_nanf("");
-    }
-    return 0.f;
+    if (__builtin_expect(l != 0.f, 1)) return l;
+    int k0, k1;
+    visible<RUN>(u, window, r, k0, k1);
+    return k0 < k1 ? 0.f : NONE;
 }
 
 // Memory of a team's slot, past the caches of the XCDs (see buffer_to_lds).
@@ -559,7 +558,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs<T>& a, float* part, in
                 visible<KEYS>(u, a.window, r, k0, k1);
                 float m, l, o[D / 64];
                 plain_row<T, D>(a, u.seq, u.h, query_of<T, D>(a, u, r), k0, k1, lane, m, l, o);
-                if (lane < TW) { sh.m[lane][r] = lane == 0 ? m : -__builtin_inff(); sh.l[lane][r] = lane == 0 ? l : 0.f; }
+                if (lane < TW) { sh.m[lane][r] = lane == 0 ? m : -__builtin_inff(); sh.l[lane][r] = lane == 0 ? l : NONE; }
 #pragma unroll
                 for (int e = 0; e < D / 64; ++e) {
                     const int d = 64 * e + lane;
@@ -571,7 +570,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs<T>& a, float* part, in
             sync();
         }
         auto finish = [&](int r, int p, const PieceSum& s) {
-            const float inv = inverse(a, u, r, s.l);
+            const float inv = inverse(s.l);
             const int64_t at = result_of(a, u, r);
             store_out4(a.out + at * D + 4 * p, f32x4{s.o[0] * inv, s.o[1] * inv, s.o[2] * inv, s.o[3] * inv});
             if (a.lse && p == 0) a.lse[at] = natural_lse(s.m, s.l);
@@ -582,7 +581,8 @@ __device__ __forceinline__ void rows_body(const PagedArgs<T>& a, float* part, in
             PieceSum ps[TW];
 #pragma unroll
             for (int w = 0; w < TW; ++w) ps[w] = PieceSum{sh.m[w][r], sh.l[w][r], *share(w, r, p)};
-            const PieceSum s = add_tree(ps);
+            PieceSum s = add_tree(ps);
+            if (!flags) s.l = sum_of<KEYS>(u, a.window, r, s.l);
             if (u.pieces == 1) {
                 finish(r, p, s);
             } else {
@@ -612,7 +612,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs<T>& a, float* part, in
                 for (int x = tid % span; x < items; x += span) {
                     if (grp >= ng) break;
                     const int r = x / P4, p = x % P4;
-                    PieceSum s{-__builtin_inff(), 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+                    PieceSum s{-__builtin_inff(), NONE, f32x4{0.f, 0.f, 0.f, 0.f}};
                     for (int i0 = grp; i0 < u.pieces; i0 += 4 * ng) {
                         u32x4 v[4];
                         u32x2 ml[4];
@@ -637,7 +637,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs<T>& a, float* part, in
                 if (ng > 1) {
                     sync();
                     if (tid < items) {
-                        PieceSum s{-__builtin_inff(), 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+                        PieceSum s{-__builtin_inff(), NONE, f32x4{0.f, 0.f, 0.f, 0.f}};
                         for (int g = 0; g < ng; ++g) {
                             const f32x4* from = (const f32x4*)smem + 2 * (g * items + tid);
                             const f32x4 ml = from[1];

@@ -428,7 +428,7 @@ void infmllm_rotary_destroy(infmllm_rotary_t* r);
  *   - a sequence with fewer cached tokens than new ones: the first of its new tokens have no position; they are not
  *     appended (their rows of q_out are left as they were), and see no key;
  *   - tokens from starts[seqs] on belong to no sequence: their rows of all outputs are left as they were.
- * Pages may be shared by sequences for reading; what two tokens of a call append to one row is one of the two.
+ * Pages may be shared by sequences for reading; what two tokens of a call append to one row may be pieces of both.
  */
 typedef struct infmllm_paged infmllm_paged_t; /* opaque, library-owned host object */
 
@@ -446,9 +446,10 @@ typedef struct infmllm_batch {
 enum {
     INFMLLM_PAGED_SCALE = 0,  /* softmax scale on q.k, > 0, scale * log2(e) a normal float; default 1/sqrt(head_dim) */
     INFMLLM_PAGED_WINDOW = 1, /* a token sees the newest `window` keys, itself included; 0 (default): all          */
-    INFMLLM_PAGED_KERNEL = 2  /* debug/test, bf16: 0 (default) = the attention picks its kernel; 1 = the one for few rows, 2 = that for
-                                 chunks, 3 = both side by side (the first for sequences of at most 16 rows).  Results are the
-                                 same up to the rounding of weights                                              */
+    INFMLLM_PAGED_KERNEL = 2  /* bf16: 0 (default) = the attention picks its kernel, for time; 1 = the one for few rows for every sequence:
+                                 softmax weights in 16 bits whatever a token is batched with (chunks take 1.4 to 3.2 times
+                                 as long).  debug/test: 2 = that for chunks, whose weights have 8 bits; 3 = both side by side, the
+                                 first for sequences of at most 16 rows (new tokens * heads / kv_heads)           */
 };
 
 /*
@@ -493,7 +494,8 @@ int infmllm_paged_append(infmllm_paged_t* p, infmllm_rotary_t* rotary, const inf
  *          dense, and must not overlap q otherwise
  *   lse    device, float [tokens][heads]: log(sum_j exp(scale * q.K[j])), -inf where no key (or none with a logit above -inf) is
  *          seen.  May be null
- * A hidden key or value reaches no result, whatever it is.  bf16: products with fp32 sums, weights of chunks rounded to bf16.
+ * A hidden key or value reaches no result, whatever it is.  bf16: products with fp32 sums; softmax weights in 16 bits for few rows, 8 for
+ * chunks (INFMLLM_PAGED_KERNEL).  The same call gives the same bits; another batch around a token may cut its keys elsewhere.
  * Errors: EINVAL (also pointers or strides that are not multiples of 16 bytes, tokens * heads / kv_heads above 2^30), ESTATE (not
  * attached), EHIP.
  */

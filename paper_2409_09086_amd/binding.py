@@ -369,7 +369,7 @@ class _Attached:
 
     Calls are enqueued on the object's HIP stream, the one that was current when it was made (or hip_stream).  Made under another current
     stream, a call is not ordered with it: that is the caller's (wait_stream); new outputs belong to the object's stream then, and tensors
-    that the call was given may be dropped at once."""
+    that the call was given may be dropped at once.  A captured graph of calls uses the workspace: it needs the object as long as it lives."""
 
     def _attach(self, prefix, handle, device, hip_stream):
         L = lib()
@@ -477,7 +477,7 @@ class PagedBatch:
 class PagedCache(_Attached):
     """infmllm_paged_t with its workspace: geometry and scratch of a paged cache; the pools of a layer, [pages, kv_heads,
     page_size, head_dim] each, are the caller's and are arguments of every call (pools() makes a pair).  Calls run on the HIP stream that was
-    current at its creation."""
+    current at its creation.  kernel=1: softmax weights of chunks in 16 bits too (INFMLLM_PAGED_KERNEL)."""
 
     def __init__(self, pages, page_size, heads, kv_heads, head_dim, dtype=torch.bfloat16, scale=None, window=None, kernel=None, device="cuda:0",
                  hip_stream=None):

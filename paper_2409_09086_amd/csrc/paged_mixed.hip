@@ -7,7 +7,7 @@
 // A compute unit by itself draws MIXED_CU_BYTES a microsecond, all of them together MIXED_BYTES, so that decoding needs no more than
 // some 140 units to be as fast as it gets.  It gets as many as make both ends finish together; where the memory is the longer end,
 // all that the chunks can do without.  us, two launches one after the other / this: 512 tokens over 4206 keys beside 31 over 512..4096, 32 heads
-// on 8, 123 / 88; 2 x 256 over 1000..2000 beside 100 161 / 128; 1024 over 4500 beside 16 over 100..8000 162 / 131; 100 over 1000..2000 beside 200
+// on 8, 123 / 88 (78 to 90 by card); 2 x 256 over 1000..2000 beside 100 161 / 128; 1024 over 4500 beside 16 over 100..8000 162 / 131; 100 over 1000..2000 beside 200
 // 270 / 222; 2048 on themselves beside 60 of one key 68 / 64.  With 40e3 and 1.7 in the place of 38e3 and 2.1: 88, 153, 129, 223, 80.
 #include <algorithm>
 #include <climits>

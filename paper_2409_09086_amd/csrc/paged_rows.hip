@@ -15,8 +15,8 @@
 // CU and more (two, if they are brief), a single wavefront, which has nobody to wait for.
 //
 // Measured: 64 tokens over 256..8192 keys of 32 heads on 8, 1.12 GB, 196 us = 5.7 TB/s, where a copy of 1 GB goes at 4.9; 512
-// tokens over 10..300 keys 82 us = 4.1 TB/s; one token over 1001 keys of 32 heads 10 us, of which 3 are the way to the first
-// keys, 2 their way, 1 the products, 3 the merges.
+// tokens over 10..300 keys 77 to 82 us, by card, = 4.1 to 4.3 TB/s; one token over 1001 keys of 32 heads 10.8 us at the least, 12.1 in the median, of
+// which 3 are the way to the first keys, 2 their way, 1 the products, 3 the merges.
 #include <algorithm>
 #include <climits>
 #include <cmath>

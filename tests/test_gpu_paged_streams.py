@@ -25,7 +25,7 @@ def made(side):
 
 
 def calls(c, cache, rot, K, V, b, q, k, v):
-    """Every call that makes or reads tensors of its own: (inputs that may be dropped, call)."""
+    """The calls that make and read tensors, by name."""
     pos = torch.arange(c.tokens, dtype=torch.int32, device=DEV)
     return {"apply": lambda: rot.apply(pos, q, k)[0], "append": lambda: cache.append(b, k, v, K, V, rotary=rot, q=q),
             "attend": lambda: cache.attend(b, q, K, V)}
